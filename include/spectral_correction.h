@@ -264,6 +264,107 @@ SC_API sc_status sc_lowrank_compress(const void* G_dev, int grad_dtype, void* E_
  * (the same start on every worker, nothing transmitted). */
 SC_API sc_status sc_lowrank_init_q(void* Q_dev, int64_t cols, int rho, uint64_t seed, void* stream);
 
+/* ---- the layer around the step: norm, linear layer, activations kept in 8 bits ---------------------------------
+ *
+ * What produces the activations and gradients the step starts from, for one pre-norm block
+ *     h = layer_norm(x)     a = act(h W1^T + b1)     y = a W2^T + b2 + x
+ * and its backward pass, with the activations that wait for the backward pass held in 8 bits. Stand-alone (no plan),
+ * asynchronous on `stream`, no device memory allocated. Matrices are row-major with a row stride (ld, in elements) of
+ * at least their width; rows of a matrix are tokens, or out features for a weight. Vectors of parameters (norm weight,
+ * biases) and their gradients are contiguous fp32. tokens = 0 is a completed call (gradients of parameters are then
+ * zero). A dimension above 2^30 is SC_ERR_TOO_LARGE; a pointer that is not a multiple of its element's size (16 bytes
+ * for checkpoints and workspaces) is SC_ERR_ALIGNMENT. */
+
+typedef enum sc_activation {
+  SC_ACT_NONE = 0,
+  SC_ACT_RELU = 1,  /* max(z, 0); slope 0 at z = 0 */
+  SC_ACT_GELU = 2,  /* z Phi(z), Phi the normal distribution function (the form with erf) */
+  SC_ACT_SILU = 3   /* z / (1 + exp(-z)) */
+} sc_activation;
+
+/* sc_layernorm_forward - y = (x - mean) * rstd * weight + bias over each row, rstd = 1 / sqrt(var + eps), var the mean
+ * squared deviation. Statistics in fp32 from the deviations themselves (not from a difference of two sums).
+ *   X, Y      device: rows x cols, dtype (sc_dtype), row strides ldx / ldy. Y may be X.
+ *   weight    device: cols fp32, or NULL (ones);   bias  device: cols fp32, or NULL (zeros)
+ *   stats     device: 2 * rows fp32, receives the means, then the rstds; or NULL
+ *   act8      device: receives Y as an 8-bit checkpoint of sc_act8_bytes(rows, cols) bytes (from the fp32 result, before
+ *             it is rounded to dtype); or NULL
+ * eps >= 0. */
+SC_API sc_status sc_layernorm_forward(const void* X_dev, int dtype, const void* weight_dev, const void* bias_dev,
+                                      float eps, void* Y_dev, void* stats_dev, void* act8_dev, int64_t rows,
+                                      int64_t cols, int64_t ldx, int64_t ldy, void* stream);
+
+/* sc_layernorm_backward - with n = (x - mean) rstd and g = dY * weight:
+ *     dX = rstd (g - mean(g) - n mean(g n)) + residual_grad        dweight = sum_rows dY n      dbias = sum_rows dY
+ *   dY, X, dX, residual_grad   device: rows x cols, dtype, row strides lddy / ldx / lddx / ldr. residual_grad (the gradient
+ *                              that reaches x around the block) may be NULL. dX may be dY or residual_grad.
+ *   stats                      device: what the forward call wrote
+ *   dweight, dbias             device: cols fp32, overwritten; either may be NULL
+ *   workspace                  device: sc_layernorm_workspace_bytes(rows, cols) bytes, 16-byte aligned (partial sums; the
+ *                              order of every sum is fixed, results repeat bit for bit) */
+SC_API size_t sc_layernorm_workspace_bytes(int64_t rows, int64_t cols);
+SC_API sc_status sc_layernorm_backward(const void* dY_dev, const void* X_dev, int dtype, const void* weight_dev,
+                                       const void* stats_dev, const void* residual_grad_dev, void* dX_dev,
+                                       void* dweight_dev, void* dbias_dev, int64_t rows, int64_t cols, int64_t lddy,
+                                       int64_t ldx, int64_t ldr, int64_t lddx, void* workspace, size_t workspace_bytes,
+                                       void* stream);
+
+/* Activations in 8 bits. Blocks of 32 neighbouring features of one token share a power of two 2^e,
+ * e = max(floor(log2(largest |x| of the block)) - 6, -126); a value is held as the integer rint(x / 2^e) (halves to even)
+ * clamped to +-127 and stands for that integer times 2^e, which bf16 represents exactly: a checkpoint that has been
+ * expanded to bf16 loses nothing. The error is at most 2^e / 2 (2^e for a value that was clamped), at most 1/64 of the
+ * block's largest value. A block that holds an infinity or a NaN stands for NaNs.
+ * Layout of a checkpoint (16-byte aligned): tokens x F int8, F = features rounded up to 32 (the padding is zero),
+ * then, from the next multiple of 256 bytes, tokens x F/32 bytes e + 127 (255: a block of NaNs). */
+SC_API size_t sc_act8_bytes(int64_t tokens, int64_t features);
+SC_API sc_status sc_act8_compress(const void* X_dev, int dtype, void* act8_dev, int64_t tokens, int64_t features,
+                                  int64_t ldx, void* stream);
+
+/* Y = act(v), v the values the checkpoint stands for (SC_ACT_NONE: v itself). */
+SC_API sc_status sc_act8_expand(const void* act8_dev, int act, void* Y_dev, int dtype, int64_t tokens, int64_t features,
+                                int64_t ldy, void* stream);
+
+/* dZ = dA * act'(v): the gradient through an activation whose argument was kept in 8 bits. dZ may be dA. */
+SC_API sc_status sc_act8_backward(const void* dA_dev, const void* act8_dev, int act, void* dZ_dev, int dtype,
+                                  int64_t tokens, int64_t features, int64_t ldda, int64_t lddz, void* stream);
+
+/* sc_linear_forward - z = X W^T + bias, Y = act(z) + residual, in one kernel.
+ *   X           device: tokens x cols, operand_dtype, row stride ldx
+ *   W           device: rows x cols, operand_dtype, row stride ldw (out features x in features)
+ *   bias        device: rows fp32, or NULL
+ *   residual    device: tokens x rows, out_dtype, row stride ldr, or NULL
+ *   Y           device: tokens x rows, out_dtype, row stride ldy; may be `residual`
+ *   act8        device: receives z (from the fp32 sum) as an 8-bit checkpoint of tokens x rows, or NULL
+ *   status_dev  device: one uint32 that receives bit 0 if a bounded device-side wait runs out, or NULL
+ * bf16 operands whose row strides are multiples of 8 and whose base is 16-byte aligned run on the tensor cores (fp32
+ * accumulation); anything else (fp32 operands, odd strides) on the CUDA cores in fp32. Widths need no alignment. */
+SC_API sc_status sc_linear_forward(const void* X_dev, const void* W_dev, int operand_dtype, const void* bias_dev,
+                                   const void* residual_dev, void* Y_dev, int out_dtype, int act, void* act8_dev,
+                                   int64_t tokens, int64_t rows, int64_t cols, int64_t ldx, int64_t ldw, int64_t ldr,
+                                   int64_t ldy, void* status_dev, void* stream);
+
+/* sc_linear_backward_input - dX = dY W, and with `act8` (a checkpoint of tokens x cols: what this layer's input was the
+ * activation of) dX = (dY W) * act'(v), the gradient of that pre-activation, in one kernel.
+ *   dY tokens x rows, W rows x cols: operand_dtype;  dX tokens x cols: out_dtype. act must be SC_ACT_NONE when act8 is NULL. */
+SC_API sc_status sc_linear_backward_input(const void* dY_dev, const void* W_dev, int operand_dtype, const void* act8_dev,
+                                          int act, void* dX_dev, int out_dtype, int64_t tokens, int64_t rows,
+                                          int64_t cols, int64_t lddy, int64_t ldw, int64_t lddx, void* status_dev,
+                                          void* stream);
+
+/* sc_linear_weight_grad - G = scale * dY^T act(v) and dbias = sum over the tokens of dY, from the layer's input (or the
+ * pre-activation it is the activation of) kept in 8 bits. act(v) is formed once, in dY's type, in the workspace.
+ * A checkpoint of masked activations (sc_apply_prf_mask) gives the masked weight gradient the step takes.
+ *   dY         device: tokens x rows, operand_dtype, row stride lddy
+ *   act8       device: checkpoint of tokens x cols
+ *   G          device: rows x cols contiguous, out_dtype, overwritten
+ *   dbias      device: rows fp32, overwritten (not multiplied by scale), or NULL
+ *   workspace  device: sc_linear_weight_grad_workspace_bytes(...) bytes, 16-byte aligned */
+SC_API size_t sc_linear_weight_grad_workspace_bytes(int operand_dtype, int64_t tokens, int64_t rows, int64_t cols);
+SC_API sc_status sc_linear_weight_grad(const void* dY_dev, int operand_dtype, const void* act8_dev, int act, float scale,
+                                       void* G_dev, int out_dtype, void* dbias_dev, int64_t tokens, int64_t rows,
+                                       int64_t cols, int64_t lddy, void* workspace, size_t workspace_bytes,
+                                       void* status_dev, void* stream);
+
 /* ---- inspection / test hooks ------------------------------------------------------------------------- */
 
 /* Copy matrix `mat`'s cached basis into caller device buffers (any may be NULL):

@@ -17,6 +17,7 @@ SC_WARN_NO_ANCHOR = 1
 SC_DTYPE_BF16, SC_DTYPE_FP32 = 0, 1
 SC_ENGINE_AUTO, SC_ENGINE_SIMT = 0, 1
 SC_OPT_ADAMW, SC_OPT_ADEMAMIX = 0, 1
+SC_ACT_NONE, SC_ACT_RELU, SC_ACT_GELU, SC_ACT_SILU = 0, 1, 2, 3
 
 
 class SCError(RuntimeError):
@@ -90,6 +91,19 @@ EXPORTS = {
     "sc_lowrank_compress": (C.c_int, [_VP, C.c_int, _VP, _VP, _VP, C.c_int64, C.c_int64, C.c_int, C.c_int, _VP, C.c_size_t,
                                       _VP]),
     "sc_lowrank_init_q": (C.c_int, [_VP, C.c_int64, C.c_int, C.c_uint64, _VP]),
+    "sc_layernorm_forward": (C.c_int, [_VP, C.c_int, _VP, _VP, C.c_float, _VP, _VP, _VP] + [C.c_int64] * 4 + [_VP]),
+    "sc_layernorm_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "sc_layernorm_backward": (C.c_int, [_VP, _VP, C.c_int, _VP, _VP, _VP, _VP, _VP, _VP] + [C.c_int64] * 6 +
+                              [_VP, C.c_size_t, _VP]),
+    "sc_act8_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "sc_act8_compress": (C.c_int, [_VP, C.c_int, _VP] + [C.c_int64] * 3 + [_VP]),
+    "sc_act8_expand": (C.c_int, [_VP, C.c_int, _VP, C.c_int] + [C.c_int64] * 3 + [_VP]),
+    "sc_act8_backward": (C.c_int, [_VP, _VP, C.c_int, _VP, C.c_int] + [C.c_int64] * 4 + [_VP]),
+    "sc_linear_forward": (C.c_int, [_VP, _VP, C.c_int, _VP, _VP, _VP, C.c_int, C.c_int, _VP] + [C.c_int64] * 7 + [_VP, _VP]),
+    "sc_linear_backward_input": (C.c_int, [_VP, _VP, C.c_int, _VP, C.c_int, _VP, C.c_int] + [C.c_int64] * 6 + [_VP, _VP]),
+    "sc_linear_weight_grad_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_int64] * 3),
+    "sc_linear_weight_grad": (C.c_int, [_VP, C.c_int, _VP, C.c_int, C.c_float, _VP, C.c_int, _VP] + [C.c_int64] * 4 +
+                              [_VP, C.c_size_t, _VP, _VP]),
     "sc_export_basis": (C.c_int, [_VP, C.c_int, _VP, _VP, _VP]),
     "sc_import_basis": (C.c_int, [_VP, C.c_int, _VP, _VP, _VP]),
     "sc_export_projection": (C.c_int, [_VP, C.c_int, _VP, _VP]),

@@ -1,0 +1,58 @@
+// The linear layer's three products (forward, input gradient, weight gradient): what the engines have in common.
+#pragma once
+
+#include "sc_act8.cuh"
+
+namespace sc {
+
+// What happens to a finished sum before it is stored.
+//   kEpiForward   z = acc + bias[col]; z -> checkpoint (if q); y = act(z) + res
+//   kEpiInput     acc * act'(value of the checkpoint) (if q), else acc
+//   kEpiWeight    acc * scale
+enum EpiKind { kEpiForward = 0, kEpiInput = 1, kEpiWeight = 2 };
+
+struct LinEpilogue {
+  void* out;                // rows of D, out_f32 ? fp32 : bf16
+  const float* bias;        // forward: one per column of D, or null
+  const void* res;          // forward: same type as out, or null
+  int8_t* q;                // forward: written; input: read; or null
+  uint8_t* e;
+  int64_t wide;             // row stride of q (e: wide / 32)
+  int64_t ldo, ldr;
+  int out_f32;
+  int act;
+  float scale;
+};
+
+// D[m x n] = sum_k A(m, k) B(n, k); element (i, k) of an operand is at base[i * s_row + k * s_k], one stride is 1.
+struct LinOperand {
+  const void* base;
+  int64_t s_row, s_k;
+};
+
+struct LinProblem {
+  LinOperand A, B;
+  int64_t M, N, K;
+  LinEpilogue epi;
+};
+
+sc_status linear_simt(int kind, int operand_f32, const LinProblem& p, cudaStream_t s);
+
+__device__ __forceinline__ float act_value_rt(int act, float z) {
+  switch (act) {
+    case SC_ACT_RELU: return act_value<SC_ACT_RELU>(z);
+    case SC_ACT_GELU: return act_value<SC_ACT_GELU>(z);
+    case SC_ACT_SILU: return act_value<SC_ACT_SILU>(z);
+    default: return z;
+  }
+}
+__device__ __forceinline__ float act_slope_rt(int act, float z) {
+  switch (act) {
+    case SC_ACT_RELU: return act_slope<SC_ACT_RELU>(z);
+    case SC_ACT_GELU: return act_slope<SC_ACT_GELU>(z);
+    case SC_ACT_SILU: return act_slope<SC_ACT_SILU>(z);
+    default: return 1.f;
+  }
+}
+
+}  // namespace sc
