@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspectral_correction.so")
 SOURCES = ["sc_plan.cu", "sc_simt.cu", "sc_tc.cu", "sc_noalloc.cu", "sc_mask.cu", "sc_wgrad.cu", "sc_lowrank.cu", "sc_fullspec.cu",
-           "sc_norm.cu", "sc_act8.cu", "sc_linear.cu"]
+           "sc_norm.cu", "sc_act8.cu", "sc_linear.cu", "sc_linear_tc.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-fvisibility=hidden", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

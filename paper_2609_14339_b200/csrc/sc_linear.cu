@@ -149,6 +149,12 @@ sc_status linear_simt(int kind, int operand_f32, const LinProblem& p, cudaStream
   }
 }
 
+// bf16 operands that TMA can describe: tensor cores; everything else: CUDA cores.
+static sc_status linear_run(int kind, int operand_f32, const LinProblem& p, unsigned* status, cudaStream_t s) {
+  if (!operand_f32 && linear_tc_supported(p)) return linear_tc(kind, p, status, s);
+  return linear_simt(kind, operand_f32, p, s);
+}
+
 }  // namespace sc
 
 using namespace sc;
@@ -181,7 +187,8 @@ extern "C" sc_status sc_linear_forward(const void* X_dev, const void* W_dev, int
     const Act8View v = act8_view(act8_dev, tokens, rows);
     p.epi.q = v.q; p.epi.e = v.e; p.epi.wide = v.wide;
   }
-  return linear_simt(kEpiForward, operand_dtype == SC_DTYPE_FP32, p, static_cast<cudaStream_t>(stream));
+  return linear_run(kEpiForward, operand_dtype == SC_DTYPE_FP32, p, static_cast<unsigned*>(status_dev),
+                    static_cast<cudaStream_t>(stream));
 }
 
 extern "C" sc_status sc_linear_backward_input(const void* dY_dev, const void* W_dev, int operand_dtype,
@@ -210,7 +217,8 @@ extern "C" sc_status sc_linear_backward_input(const void* dY_dev, const void* W_
     const Act8View v = act8_view(const_cast<void*>(act8_dev), tokens, cols);
     p.epi.q = v.q; p.epi.e = v.e; p.epi.wide = v.wide;
   }
-  return linear_simt(kEpiInput, operand_dtype == SC_DTYPE_FP32, p, static_cast<cudaStream_t>(stream));
+  return linear_run(kEpiInput, operand_dtype == SC_DTYPE_FP32, p, static_cast<unsigned*>(status_dev),
+                    static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t sc_linear_weight_grad_workspace_bytes(int operand_dtype, int64_t tokens, int64_t rows, int64_t cols) {
@@ -263,5 +271,8 @@ extern "C" sc_status sc_linear_weight_grad(const void* dY_dev, int operand_dtype
   p.epi.ldo = cols;
   p.epi.out_f32 = out_dtype == SC_DTYPE_FP32;
   p.epi.scale = scale;
-  return linear_simt(kEpiWeight, operand_dtype == SC_DTYPE_FP32, p, s);
+  if (tokens == 0)
+    return cudaMemsetAsync(G_dev, 0, (size_t)rows * (size_t)cols * (out_dtype == SC_DTYPE_FP32 ? 4 : 2), s) == cudaSuccess
+               ? SC_OK : SC_ERR_CUDA;
+  return linear_run(kEpiWeight, operand_dtype == SC_DTYPE_FP32, p, static_cast<unsigned*>(status_dev), s);
 }

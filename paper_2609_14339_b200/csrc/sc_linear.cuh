@@ -36,6 +36,10 @@ struct LinProblem {
   LinEpilogue epi;
 };
 
+// Tensor-core engine: bf16 operands that TMA can describe (16-byte aligned base and row stride).
+bool linear_tc_supported(const LinProblem& p);
+sc_status linear_tc(int kind, const LinProblem& p, unsigned* status, cudaStream_t s);
+
 sc_status linear_simt(int kind, int operand_f32, const LinProblem& p, cudaStream_t s);
 
 __device__ __forceinline__ float act_value_rt(int act, float z) {

@@ -1,0 +1,736 @@
+// Tensor-core engine of the linear layer's three products (see sc_linear.cu for the roles of A and B):
+//   D[m, n] = sum_k A(m, k) B(n, k),  bf16 operands, fp32 accumulation in tensor memory, epilogue fused.
+//
+// linear_pair_kernel    large products: a cluster of two SMs on a 256 x bn tile (tcgen05 cta_group::2), persistent, two
+//                       accumulators in tensor memory so that a tile's epilogue runs under the next tile's MMAs.
+// linear_split_kernel   few rows of D, or few tiles: one SM on a 128 x bn tile of D^T (the contiguous dimension of D on the
+//                       128 accumulator lanes), the contraction split over a cluster of up to 8 blocks that join their
+//                       partial sums through distributed shared memory in a fixed order.
+//
+// Operands come by TMA in boxes of 64 along k, 128-byte swizzle; an operand whose contraction index is slow in memory is
+// taken as it lies (MN-major descriptor), nothing is transposed. Sizes that end inside a box come in as zeros.
+// Every mbarrier wait is bounded; a wait that runs out latches the time-out bit in *status and the block winds down.
+#include <cuda.h>
+
+#include "sc_linear.cuh"
+#include "sc_ptx.cuh"
+
+namespace sc {
+namespace {
+
+constexpr int kLtK = 64;                       // contraction per pipeline stage
+constexpr int kLtBox = 64 * kLtK * 2;          // one 64 x 64 bf16 box: 8 KB
+constexpr int kLtPairStages = 6;
+constexpr int kLtMaxStages = 8;
+constexpr int kLtPairThreads = 320;            // producer, issuer, 8 epilogue warps
+constexpr int kLtSplitThreads = 192;           // producer, issuer, 4 epilogue warps
+
+struct LtShape {
+  int M, N;                // D is M x N
+  int kchunks;
+  int bn;                  // tile width: columns of D (pair), rows of D (split)
+  int tiles_m, tiles_n;    // pair: 256-row x bn-column tiles of D; split: bn-row x 128-column tiles of D
+  int m_fastest;           // pair: which way consecutive tiles run
+  int stages;              // split
+  int vec;                 // out and res take 16-byte accesses
+  int vec_bias;
+};
+
+struct LtBars {
+  uint64_t full[kLtMaxStages], empty[kLtMaxStages];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t drain;                // abort path only: the leader's MMAs in flight have finished
+  uint32_t tmem_slot;
+  int abort_flag;
+  int never_flag;
+};
+
+template <int KIND>
+struct Layout {                  // contraction index slow in memory?
+  static constexpr bool a_mn = KIND == kEpiWeight, b_mn = KIND != kEpiForward;
+};
+
+__device__ __forceinline__ uint64_t lt_desc(uint32_t saddr, bool mn, int k16) {
+  return mn ? umma_desc_mn_bf16(saddr + k16 * 2048, kLtBox) : umma_desc_k128(saddr + k16 * 32);
+}
+
+// ---------------------------------------------------------------------------------------- epilogue, one row per thread
+__device__ __forceinline__ void load8(const void* p, int f32, int64_t i, bool vec, int n, float* r) {
+  if (vec && n >= 8) {
+    if (f32) {
+      const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+      const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i + 4);
+      r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w; r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
+    } else {
+      const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + i);
+      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { r[2 * j] = __uint_as_float(w[j] << 16); r[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      r[j] = j < n ? (f32 ? static_cast<const float*>(p)[i + j] : __bfloat162float(static_cast<const bf16*>(p)[i + j])) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(void* p, int f32, int64_t i, bool vec, int n, const float* v) {
+  if (vec && n >= 8) {
+    if (f32) {
+      float* o = static_cast<float*>(p) + i;
+      *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+        w[j] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      *reinterpret_cast<uint4*>(static_cast<bf16*>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) {
+        if (f32) static_cast<float*>(p)[i + j] = v[j];
+        else static_cast<bf16*>(p)[i + j] = __float2bfloat16_rn(v[j]);
+      }
+  }
+}
+
+template <int N_, typename F>
+__device__ __forceinline__ void each(float* v, F f) {
+#pragma unroll
+  for (int j = 0; j < N_; ++j) v[j] = f(v[j]);
+}
+// the activation is uniform over the launch: one branch per block of values
+template <int N_>
+__device__ __forceinline__ void act_values(int act, float* v) {
+  switch (act) {
+    case SC_ACT_RELU: each<N_>(v, [](float z) { return act_value<SC_ACT_RELU>(z); }); break;
+    case SC_ACT_GELU: each<N_>(v, [](float z) { return act_value<SC_ACT_GELU>(z); }); break;
+    case SC_ACT_SILU: each<N_>(v, [](float z) { return act_value<SC_ACT_SILU>(z); }); break;
+    default: break;
+  }
+}
+template <int N_>
+__device__ __forceinline__ void act_slopes(int act, float* v) {
+  switch (act) {
+    case SC_ACT_RELU: each<N_>(v, [](float z) { return act_slope<SC_ACT_RELU>(z); }); break;
+    case SC_ACT_GELU: each<N_>(v, [](float z) { return act_slope<SC_ACT_GELU>(z); }); break;
+    case SC_ACT_SILU: each<N_>(v, [](float z) { return act_slope<SC_ACT_SILU>(z); }); break;
+    default: each<N_>(v, [](float) { return 1.f; });
+  }
+}
+
+// 32 neighbouring columns (from a multiple of 32) of one row: v holds the sums
+template <int KIND>
+__device__ __forceinline__ void epilogue_row32(const LinEpilogue& e, const LtShape& sh, const float* aux, float* v,
+                                               int64_t row, int col) {
+  const int left = sh.N - col;             // > 0
+  if (KIND == kEpiForward) {
+    if (e.bias) {
+      if (sh.vec_bias && left >= 32) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          const float4 b = __ldg(reinterpret_cast<const float4*>(e.bias + col + j));
+          v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j < left) v[j] += __ldg(e.bias + col + j);
+      }
+    }
+    if (e.q) {
+      if (left < 32) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j >= left) v[j] = 0.f;
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+      const uint32_t eb = a8_scale_byte(top);
+      const float inv = a8_inverse(eb);
+      uint4* q = reinterpret_cast<uint4*>(e.q + row * e.wide + col);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float* x = v + 16 * h;
+        q[h] = make_uint4(a8_pack4(x[0], x[1], x[2], x[3], inv), a8_pack4(x[4], x[5], x[6], x[7], inv),
+                          a8_pack4(x[8], x[9], x[10], x[11], inv), a8_pack4(x[12], x[13], x[14], x[15], inv));
+      }
+      e.e[row * (e.wide / 32) + col / 32] = (uint8_t)eb;
+    }
+    act_values<32>(e.act, v);
+    if (e.res) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] += aux[j];
+    }
+  } else if (KIND == kEpiInput) {
+    if (e.q) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] *= aux[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] *= e.scale;
+  }
+#pragma unroll
+  for (int j = 0; j < 32; j += 8)
+    if (j < left) store8(e.out, e.out_f32, row * e.ldo + col + j, sh.vec, left - j, v + j);
+}
+// what the epilogue needs besides the sums, read before the sums are waited for: residual, or slopes of the checkpoint
+template <int KIND>
+__device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtShape& sh, float* aux, int64_t row, int col) {
+  const int left = sh.N - col;
+  if (KIND == kEpiForward && e.res) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) load8(e.res, e.out_f32, row * e.ldr + col + j, sh.vec, left - j, aux + j);
+  } else if (KIND == kEpiInput && e.q) {
+    const uint4* q = reinterpret_cast<const uint4*>(e.q + row * e.wide + col);
+    const uint4 a = q[0], b = q[1];
+    const float step = a8_step(e.e[row * (e.wide / 32) + col / 32]);
+    a8_unpack4(a.x, step, aux); a8_unpack4(a.y, step, aux + 4); a8_unpack4(a.z, step, aux + 8); a8_unpack4(a.w, step, aux + 12);
+    a8_unpack4(b.x, step, aux + 16); a8_unpack4(b.y, step, aux + 20); a8_unpack4(b.z, step, aux + 24); a8_unpack4(b.w, step, aux + 28);
+    act_slopes<32>(e.act, aux);
+  }
+}
+
+// ---------------------------------------------------------------------------------------- two SMs per 256 x bn tile
+template <int KIND>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLtPairThreads, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const __grid_constant__ LtShape sh, const __grid_constant__ LinEpilogue epi, unsigned* status) {
+  constexpr bool a_mn = Layout<KIND>::a_mn, b_mn = Layout<KIND>::b_mn;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  LtBars* bars = reinterpret_cast<LtBars*>(smem + kLtPairStages * 4 * kLtBox);
+  volatile int* abort_flag = &bars->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int tiles = sh.tiles_m * sh.tiles_n, half = sh.bn / 2;
+  const int b_boxes = (half + 63) / 64;
+  const uint32_t stage_bytes = 2 * kLtBox + (b_mn ? b_boxes * kLtBox : half * 128);     // what TMA writes per block
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kLtPairStages; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(&bars->acc_full[a], 1); mbar_init(&bars->acc_empty[a], 16); }
+    mbar_init(&bars->drain, 1);
+    bars->abort_flag = 0;
+    bars->never_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();            // the peer's barriers exist before anything is sent to them
+  tc_fence_after();
+  const uint32_t tmem_base = bars->tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool dead = false;
+      for (int tile = pair; tile < tiles && !dead; tile += n_pairs) {
+        const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
+        const int a_row = tm * 256 + (int)rank * 128, b_row = tn * sh.bn + (int)rank * half;
+        for (int kc = 0; kc < sh.kchunks; ++kc, ++it) {
+          const int s = it % kLtPairStages;
+          if (!mbar_wait(&bars->empty[s], ((it / kLtPairStages) & 1) ^ 1, abort_flag)) { dead = true; break; }
+          uint8_t* st = smem + (size_t)s * 4 * kLtBox;
+          if (rank == 0) mbar_expect_tx(&bars->full[s], 2 * stage_bytes);      // both blocks' bytes
+          const uint32_t leader_bar = map_to_rank(smem_u32(&bars->full[s]), 0);
+          if (a_mn) {
+            for (int b = 0; b < 2; ++b) tma_load_2d_pair(st + b * kLtBox, &map_a, leader_bar, a_row + b * 64, kc * kLtK);
+          } else {
+            tma_load_2d_pair(st, &map_a, leader_bar, kc * kLtK, a_row);
+          }
+          if (b_mn) {
+            for (int b = 0; b < b_boxes; ++b)
+              tma_load_2d_pair(st + (2 + b) * kLtBox, &map_b, leader_bar, b_row + b * 64, kc * kLtK);
+          } else {
+            tma_load_2d_pair(st + 2 * kLtBox, &map_b, leader_bar, kc * kLtK, b_row);
+          }
+        }
+      }
+      if (dead) {
+        if (status) atomicOr(status, kDevTimeout);
+        *abort_flag = 1;
+        // Let the copies in flight land before the pair's shared memory goes away: the leader, on whose barriers both
+        // blocks' bytes count, waits (bounded) for the stages it armed; the other block cannot see its own copies land
+        // and idles far longer than a copy takes. Both meet in the cluster barrier at the end.
+        if (rank == 0) {
+          for (uint32_t u = it > (uint32_t)kLtPairStages ? it - kLtPairStages : 0; u < it; ++u)
+            mbar_wait(&bars->full[u % kLtPairStages], (u / kLtPairStages) & 1, &bars->never_flag);
+        } else {
+          for (int i = 0; i < 64; ++i) __nanosleep(1000);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = umma_idesc_bf16_any(256, sh.bn, a_mn, b_mn);
+      uint32_t it = 0, t = 0;
+      bool dead = false;
+      for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
+        const uint32_t ab = t & 1;
+        if (!mbar_wait(&bars->acc_empty[ab], ((t >> 1) & 1) ^ 1, abort_flag)) { dead = true; break; }
+        tc_fence_after();
+        const uint32_t d = tmem_base + ab * 256;
+        for (int kc = 0; kc < sh.kchunks; ++kc, ++it) {
+          const int s = it % kLtPairStages;
+          if (!mbar_wait(&bars->full[s], (it / kLtPairStages) & 1, abort_flag)) { dead = true; break; }
+          tc_fence_after();
+          const uint32_t a0 = smem_u32(smem + (size_t)s * 4 * kLtBox), b0 = a0 + 2 * kLtBox;
+#pragma unroll
+          for (int k = 0; k < kLtK / 16; ++k)
+            umma_bf16_pair(d, lt_desc(a0, a_mn, k), lt_desc(b0, b_mn, k), idesc, (kc | k) != 0);
+          umma_commit_pair(&bars->empty[s]);
+        }
+        if (dead) break;
+        umma_commit_pair(&bars->acc_full[ab]);
+      }
+      if (dead) {
+        if (status) atomicOr(status, kDevTimeout);
+        *abort_flag = 1;
+        // MMAs already issued still read shared memory and write TMEM of both blocks: wait (bounded) until they are done
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];"
+                     ::"r"(smem_u32(&bars->drain)) : "memory");
+        mbar_wait(&bars->drain, 0, &bars->never_flag);
+      }
+    }
+    __syncwarp();
+  } else {
+    const int q = warp & 3, part = (warp - 2) >> 2;      // lanes of this warp's quarter; every second block of 32 columns
+    uint32_t t = 0;
+    bool dead = false;
+    for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
+      const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
+      const uint32_t ab = t & 1;
+      if (!mbar_wait(&bars->acc_full[ab], (t >> 1) & 1, abort_flag)) { dead = true; break; }
+      tc_fence_after();
+      const int row = tm * 256 + (int)rank * 128 + q * 32 + lane;
+      const uint32_t d = tmem_base + ab * 256 + ((uint32_t)(q * 32) << 16);
+      for (int c = part * 32; c < sh.bn; c += 64) {
+        const int col = tn * sh.bn + c;
+        const bool live = row < sh.M && col < sh.N;
+        float v[32], aux[32];
+        if (live) epilogue_aux32<KIND>(epi, sh, aux, row, col);
+        __syncwarp();
+        tmem_ld32(d + c, v);
+        tmem_ld_wait();
+        if (live) epilogue_row32<KIND>(epi, sh, aux, v, row, col);
+        __syncwarp();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&bars->acc_empty[ab]), 0));   // the leader's barrier
+    }
+    if (dead && lane == 0) {
+      if (status) atomicOr(status, kDevTimeout);
+      *abort_flag = 1;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();            // nothing of the peer is touched after this
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+}
+
+// ---------------------------------------------------------------------------------------- split contraction
+// One column of D (a lane of the accumulator) per thread, `count` rows of D at a time.
+template <int KIND, int CNT>
+__device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtShape& sh, float* v, int64_t row0, int col,
+                                                 float bias, int lane) {
+  const bool inside = col < sh.N;
+  float aux[CNT];
+  if (KIND == kEpiForward && e.res) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) {
+      const int64_t i = (row0 + j) * e.ldr + col;
+      aux[j] = !(inside && row0 + j < sh.M) ? 0.f
+               : e.out_f32                  ? static_cast<const float*>(e.res)[i]
+                                            : __bfloat162float(static_cast<const bf16*>(e.res)[i]);
+    }
+  } else if (KIND == kEpiInput && e.q) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) {
+      const bool ok = inside && row0 + j < sh.M;
+      aux[j] = ok ? (float)e.q[(row0 + j) * e.wide + col] * a8_step(e.e[(row0 + j) * (e.wide / 32) + col / 32]) : 0.f;
+    }
+    act_slopes<CNT>(e.act, aux);
+  }
+  if (KIND == kEpiForward) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) v[j] = inside ? v[j] + bias : 0.f;
+    if (e.q) {                    // a block of 32 columns is the 32 lanes of this warp
+#pragma unroll
+      for (int j = 0; j < CNT; ++j) {
+        const uint32_t eb = a8_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[j]) & 0x7fffffffu));
+        const float inv = a8_inverse(eb);
+        if (row0 + j < sh.M && col < e.wide) {
+          e.q[(row0 + j) * e.wide + col] = (int8_t)(inv == 0.f ? 0u : a8_round(v[j], inv) & 255u);
+          if (lane == 0) e.e[(row0 + j) * (e.wide / 32) + col / 32] = (uint8_t)eb;
+        }
+      }
+    }
+    act_values<CNT>(e.act, v);
+    if (e.res) {
+#pragma unroll
+      for (int j = 0; j < CNT; ++j) v[j] += aux[j];
+    }
+  } else if (KIND == kEpiInput) {
+    if (e.q) {
+#pragma unroll
+      for (int j = 0; j < CNT; ++j) v[j] *= aux[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) v[j] *= e.scale;
+  }
+  if (inside) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) {
+      if (row0 + j < sh.M) {
+        const int64_t i = (row0 + j) * e.ldo + col;
+        if (e.out_f32) static_cast<float*>(e.out)[i] = v[j];
+        else static_cast<bf16*>(e.out)[i] = __float2bfloat16_rn(v[j]);
+      }
+    }
+  }
+}
+
+// map_l: the operand indexed by D's columns (accumulator lanes), map_r: the one indexed by D's rows.
+template <int KIND>
+__global__ void __launch_bounds__(kLtSplitThreads)
+linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_r,
+                    const __grid_constant__ LtShape sh, const __grid_constant__ LinEpilogue epi, int split,
+                    unsigned* status) {
+  constexpr bool l_mn = Layout<KIND>::b_mn, r_mn = Layout<KIND>::a_mn;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const int r_boxes = (sh.bn + 63) / 64;
+  const uint32_t r_bytes = r_mn ? r_boxes * kLtBox : sh.bn * 128;
+  const uint32_t stage_bytes = 2 * kLtBox + r_bytes;
+  LtBars* bars = reinterpret_cast<LtBars*>(smem + (size_t)sh.stages * stage_bytes);
+  volatile int* abort_flag = &bars->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = (int)(blockIdx.x % split), tile = (int)(blockIdx.x / split);
+  const int tn = tile % sh.tiles_n, tm = tile / sh.tiles_n;
+  const int k_begin = (int)((int64_t)sh.kchunks * part / split), k_end = (int)((int64_t)sh.kchunks * (part + 1) / split);
+  int cols_tmem = 32;
+  while (cols_tmem < sh.bn) cols_tmem *= 2;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < sh.stages; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+    mbar_init(&bars->acc_full[0], 1);
+    bars->abort_flag = 0;
+    bars->never_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  if (warp == 1) tmem_alloc(&bars->tmem_slot, cols_tmem);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = bars->tmem_slot;
+
+  bool dead = false;
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      for (int kc = k_begin; kc < k_end; ++kc, ++it) {
+        const int s = it % sh.stages;
+        if (!mbar_wait(&bars->empty[s], ((it / sh.stages) & 1) ^ 1, abort_flag)) { dead = true; break; }
+        uint8_t* st = smem + (size_t)s * stage_bytes;
+        mbar_expect_tx(&bars->full[s], stage_bytes);
+        if (l_mn) {
+          for (int b = 0; b < 2; ++b) tma_load_2d(st + b * kLtBox, &map_l, &bars->full[s], tn * 128 + b * 64, kc * kLtK);
+        } else {
+          tma_load_2d(st, &map_l, &bars->full[s], kc * kLtK, tn * 128);
+        }
+        if (r_mn) {
+          for (int b = 0; b < r_boxes; ++b)
+            tma_load_2d(st + (2 + b) * kLtBox, &map_r, &bars->full[s], tm * sh.bn + b * 64, kc * kLtK);
+        } else {
+          tma_load_2d(st + 2 * kLtBox, &map_r, &bars->full[s], kc * kLtK, tm * sh.bn);
+        }
+      }
+      if (dead) {
+        if (status) atomicOr(status, kDevTimeout);
+        *abort_flag = 1;
+        for (uint32_t u = it > (uint32_t)sh.stages ? it - sh.stages : 0; u < it; ++u)
+          mbar_wait(&bars->full[u % sh.stages], (u / sh.stages) & 1, &bars->never_flag);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = umma_idesc_bf16_any(128, sh.bn, l_mn, r_mn);
+      uint32_t it = 0;
+      for (int kc = k_begin; kc < k_end; ++kc, ++it) {
+        const int s = it % sh.stages;
+        if (!mbar_wait(&bars->full[s], (it / sh.stages) & 1, abort_flag)) { dead = true; break; }
+        tc_fence_after();
+        const uint32_t l0 = smem_u32(smem + (size_t)s * stage_bytes), r0 = l0 + 2 * kLtBox;
+#pragma unroll
+        for (int k = 0; k < kLtK / 16; ++k)
+          umma_bf16(tmem_base, lt_desc(l0, l_mn, k), lt_desc(r0, r_mn, k), idesc, (kc > k_begin || k > 0) ? 1u : 0u);
+        umma_commit(&bars->empty[s]);
+      }
+      umma_commit(&bars->acc_full[0]);       // on the way out of a dead loop too: MMAs in flight have to finish
+      if (dead) {
+        if (status) atomicOr(status, kDevTimeout);
+        *abort_flag = 1;
+        mbar_wait(&bars->acc_full[0], 0, &bars->never_flag);
+      }
+    }
+    __syncwarp();
+  }
+
+  const int q = warp & 3;
+  const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16);
+  const int col = tn * 128 + q * 32 + lane;
+  const float bias = KIND == kEpiForward && epi.bias && col < sh.N ? epi.bias[col] : 0.f;
+  const int64_t row0 = (int64_t)tm * sh.bn;
+  if (split == 1) {
+    if (warp >= 2) {
+      dead = !mbar_wait(&bars->acc_full[0], 0, abort_flag);
+      tc_fence_after();
+      for (int c = 0; c < sh.bn && !dead && row0 + c < sh.M; c += 16) {
+        float v[16];
+        tmem_ld16(d + c, v);
+        tmem_ld_wait();
+        epilogue_columns<KIND, 16>(epi, sh, v, row0 + c, col, bias, lane);
+        __syncwarp();
+      }
+    }
+  } else {
+    // join: every block lays its partial sums in its own shared memory (the pipeline's, which is idle by now), then
+    // sums its share of the tile's rows over the blocks of the cluster in their order
+    float* mine = reinterpret_cast<float*>(smem);
+    if (warp >= 2) {
+      dead = !mbar_wait(&bars->acc_full[0], 0, abort_flag);
+      tc_fence_after();
+      for (int c = 0; c < sh.bn && !dead; c += 16) {
+        float v[16];
+        tmem_ld16(d + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mine[(c + j) * 128 + q * 32 + lane] = v[j];
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();
+    if (warp >= 2 && !dead) {
+      const int share = (sh.bn + split - 1) / split, first = part * share;
+      const int last = first + share < sh.bn ? first + share : sh.bn;
+      const uint32_t base = smem_u32(mine) + (q * 32 + lane) * 4;
+      for (int c = first; c < last && row0 + c < sh.M; c += 4) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < split; ++s) {
+          const uint32_t from = map_to_rank(base, s);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (c + j < last) v[j] += ld_shared_cluster(from + (c + j) * 512);
+        }
+        // the rows past this block's share belong to the next block: give them a row outside D
+        LtShape mine_sh = sh;
+        mine_sh.M = row0 + last < sh.M ? (int)(row0 + last) : sh.M;
+        epilogue_columns<KIND, 4>(epi, mine_sh, v, row0 + c, col, bias, lane);
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();            // the peers have read this block's sums
+  }
+  if (dead && lane == 0 && warp >= 2) {
+    if (status) atomicOr(status, kDevTimeout);
+    *abort_flag = 1;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem_base, cols_tmem);
+}
+
+// ---------------------------------------------------------------------------------------- host
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+
+// outer x inner bf16 matrix -> boxes of 64 (inner) x box_outer, 128-byte swizzle
+bool encode(CUtensorMap* out, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+  cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+  cuuint32_t box[2] = {64, (cuuint32_t)box_outer};
+  cuuint32_t estr[2] = {1, 1};
+  return enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// operand of `rows` x K: k fast -> boxes of `box_rows` rows, otherwise boxes of 64 rows x 64
+bool encode_operand(CUtensorMap* out, const LinOperand& o, int64_t rows, int64_t K, int box_rows) {
+  return o.s_k == 1 ? encode(out, o.base, K, rows, o.s_row, box_rows) : encode(out, o.base, rows, K, o.s_k, kLtK);
+}
+
+struct Device {
+  int n_sm = 0;
+  bool ready = false;
+};
+constexpr int kMaxDevices = 64;
+
+size_t pair_smem() { return (size_t)kLtPairStages * 4 * kLtBox + sizeof(LtBars) + 1024; }
+constexpr size_t kSplitSmemMax = 227 * 1024;
+
+// SM count of the current device, with the kernels' shared-memory limits raised on it (once per device)
+int device_sms() {
+  static Device devices[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  Device& d = devices[dev];
+  if (!d.ready) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    const int pair = (int)pair_smem(), split = (int)kSplitSmemMax;
+    const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    if (cudaFuncSetAttribute(linear_pair_kernel<kEpiForward>, at, pair) != cudaSuccess ||
+        cudaFuncSetAttribute(linear_pair_kernel<kEpiInput>, at, pair) != cudaSuccess ||
+        cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight>, at, pair) != cudaSuccess ||
+        cudaFuncSetAttribute(linear_split_kernel<kEpiForward>, at, split) != cudaSuccess ||
+        cudaFuncSetAttribute(linear_split_kernel<kEpiInput>, at, split) != cudaSuccess ||
+        cudaFuncSetAttribute(linear_split_kernel<kEpiWeight>, at, split) != cudaSuccess)
+      return 0;
+    d.n_sm = n;
+    d.ready = true;            // a second thread that gets here first does the same work to the same end
+  }
+  return d.n_sm;
+}
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Choice {
+  bool pair = false;
+  int bn = 0, split = 1, stages = 0;
+  double cost = 1e30;
+};
+
+// Clocks of the two kernels for one shape, counted from what bounds a stage: the tensor pipe (2 clocks per column of the
+// tile and stage of 64) or shared memory (each operand byte is written once and read once, 128 bytes a clock).
+Choice choose(int kind, int64_t M, int64_t N, int64_t K, int n_sm) {
+  const int64_t chunks = up(K, kLtK);
+  Choice best;
+  for (int bn = 256; bn >= 128; bn -= 32) {
+    const double tiles = (double)up(M, 256) * (double)up(N, bn), waves = (double)(int64_t)((tiles + n_sm / 2 - 1) / (n_sm / 2));
+    const double stage = 2.0 * bn > 2.0 * (128 + bn / 2) ? 2.0 * bn : 2.0 * (128 + bn / 2);
+    const double cost = waves * (double)chunks * stage * 1.1 + 4000.0 + 3000.0;
+    if (cost < best.cost) best = {true, bn, 1, kLtPairStages, cost};
+  }
+  const bool r_mn = kind == kEpiWeight;
+  const int64_t m16 = up(M, 16) * 16;
+  for (int bn = r_mn ? 64 : 16; bn <= 256; bn += r_mn ? 64 : 16) {
+    if (bn > m16 && bn > (r_mn ? 64 : 16) && bn - (r_mn ? 64 : 16) >= m16) break;
+    const size_t stage_bytes = 2 * kLtBox + (size_t)bn * 128;
+    const int per_sm = bn <= 64 ? 2 : 1;
+    int stages = (int)(((per_sm == 2 ? 110 : 220) * 1024) / stage_bytes);
+    if (stages > kLtMaxStages) stages = kLtMaxStages;
+    for (int split = 1; split <= 8; ++split) {
+      if (split > chunks) break;
+      if (split > 1 && (size_t)bn * 512 > (size_t)stages * stage_bytes) break;       // the partial sums' room
+      const double blocks = (double)up(M, bn) * (double)up(N, 128) * split;
+      const double waves = (double)(int64_t)((blocks + n_sm - 1) / n_sm);
+      const double stage = 2.0 * (128 + bn);
+      const double cost = waves * ((double)up(chunks, split) * stage + 1500.0 + 12.0 * bn / split) + (split > 1 ? 1500.0 + 8.0 * bn : 0.0) + 2000.0;
+      if (cost < best.cost) best = {false, bn, split, stages, cost};
+    }
+  }
+  return best;
+}
+
+template <int KIND>
+sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
+  const int n_sm = device_sms();
+  if (n_sm < 2) return SC_ERR_CUDA;
+  const Choice c = choose(KIND, p.M, p.N, p.K, n_sm);
+  LtShape sh{};
+  sh.M = (int)p.M; sh.N = (int)p.N;
+  sh.kchunks = (int)up(p.K, kLtK);
+  sh.bn = c.bn;
+  sh.stages = c.stages;
+  const int es = p.epi.out_f32 ? 4 : 2;
+  const auto wide = [es](const void* q, int64_t ld) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0 && (ld * es) % 16 == 0; };
+  sh.vec = wide(p.epi.out, p.epi.ldo) && (!p.epi.res || wide(p.epi.res, p.epi.ldr));
+  sh.vec_bias = (reinterpret_cast<uintptr_t>(p.epi.bias) & 15) == 0;
+  CUtensorMap a, b;
+  if (c.pair) {
+    sh.tiles_m = (int)up(p.M, 256);
+    sh.tiles_n = (int)up(p.N, c.bn);
+    if ((int64_t)sh.tiles_m * sh.tiles_n > 0x7fffffff) return SC_ERR_TOO_LARGE;
+    sh.m_fastest = p.M <= p.N;
+    if (!encode_operand(&a, p.A, p.M, p.K, 128) || !encode_operand(&b, p.B, p.N, p.K, c.bn / 2)) return SC_ERR_CUDA;
+    const int64_t tiles = (int64_t)sh.tiles_m * sh.tiles_n;
+    const int pairs = tiles < n_sm / 2 ? (int)tiles : n_sm / 2;
+    linear_pair_kernel<KIND><<<2 * pairs, kLtPairThreads, pair_smem(), s>>>(a, b, sh, p.epi, status);
+  } else {
+    sh.tiles_m = (int)up(p.M, c.bn);
+    sh.tiles_n = (int)up(p.N, 128);
+    const int64_t blocks = (int64_t)sh.tiles_m * sh.tiles_n * c.split;
+    if (blocks > 0x7fffffff) return SC_ERR_TOO_LARGE;
+    if (!encode_operand(&a, p.A, p.M, p.K, c.bn) || !encode_operand(&b, p.B, p.N, p.K, 128)) return SC_ERR_CUDA;
+    const size_t r_bytes = KIND == kEpiWeight ? (size_t)up(c.bn, 64) * kLtBox : (size_t)c.bn * 128;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kLtSplitThreads);
+    cfg.dynamicSmemBytes = (size_t)c.stages * (2 * kLtBox + r_bytes) + sizeof(LtBars) + 1024;
+    cfg.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)c.split;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, linear_split_kernel<KIND>, b, a, sh, p.epi, c.split, status) != cudaSuccess) return SC_ERR_CUDA;
+  }
+  ++g_kernel_launches;
+  return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
+}
+
+}  // namespace
+
+bool linear_tc_supported(const LinProblem& p) {
+  const auto ok = [](const LinOperand& o) {
+    const int64_t ld = o.s_k == 1 ? o.s_row : o.s_k;
+    return (reinterpret_cast<uintptr_t>(o.base) & 15) == 0 && ld % 8 == 0 && ld < (1ll << 38);
+  };
+  return ok(p.A) && ok(p.B);
+}
+
+sc_status linear_tc(int kind, const LinProblem& p, unsigned* status, cudaStream_t s) {
+  switch (kind) {
+    case kEpiForward: return launch<kEpiForward>(p, status, s);
+    case kEpiInput: return launch<kEpiInput>(p, status, s);
+    default: return launch<kEpiWeight>(p, status, s);
+  }
+}
+
+}  // namespace sc

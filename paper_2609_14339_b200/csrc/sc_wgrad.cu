@@ -40,12 +40,6 @@ struct WgBars {
   int never_flag;
 };
 
-// MN-major bf16 operand, 128-byte swizzle: atoms of 64 (MN, contiguous 128 bytes) x 8 (K rows); consecutive K groups
-// of 8 rows are 1024 bytes apart (SBO), consecutive 64-wide MN blocks `lbo` bytes apart.
-__device__ __forceinline__ uint64_t umma_desc_mn_bf16(uint32_t saddr, uint32_t lbo) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
 // bf16 x bf16 -> fp32, both operands MN-major, M = 128.
 __device__ __forceinline__ uint32_t umma_idesc_bf16_mn(int N) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(N >> 3) << 17) |
