@@ -5,50 +5,155 @@
 namespace sc {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ float ld1(const T* p) { return (float)*p; }
-template <typename T>
-__device__ __forceinline__ T cvt(float v);
-template <>
-__device__ __forceinline__ float cvt<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ bf16 cvt<bf16>(float v) { return __float2bfloat16_rn(v); }
+constexpr int kA8Unroll = 4;
 
-// one warp per block of 32 features
-template <typename T>
-__global__ void __launch_bounds__(256)
-a8_compress_kernel(const T* __restrict__ X, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int64_t wide,
-                   int64_t tokens, int64_t features, int64_t ldx) {
-  const int lane = threadIdx.x & 31;
-  const int64_t per_row = wide / 32, total = tokens * per_row;
-  for (int64_t b = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); b < total; b += (int64_t)gridDim.x * 8) {
-    const int64_t t = b / per_row, c = (b - t * per_row) * 32 + lane;
-    const float x = c < features ? ld1(X + t * ldx + c) : 0.f;
-    const uint32_t e = a8_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu));
-    const float inv = a8_inverse(e);
-    q[t * wide + c] = (int8_t)(inv == 0.f ? 0u : a8_round(x, inv) & 255u);
-    if (lane == 0) qe[b] = (uint8_t)e;
+// Work is cut into units of 8 features (four neighbouring lanes hold a block of 32). A thread takes kA8Unroll units at a
+// time, all of them loaded before the first is used: HBM latency times bandwidth is some 45 KB per SM, and one unit per
+// thread in flight leaves much of it idle.
+// FLAT: no row ends inside a unit's block and rows follow one another without a gap in the tensor and the checkpoint, so
+// the unit's number is all that is needed; otherwise row and column advance from unit to unit without a division.
+template <bool FLAT>
+struct A8Walk {
+  int64_t row, unit, step;
+  int col8, step_col8, units_row;
+  int64_t step_row;
+  __device__ A8Walk(int64_t wide) {
+    unit = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    step = (int64_t)gridDim.x * blockDim.x;
+    if (!FLAT) {
+      units_row = (int)(wide / 8);
+      row = unit / units_row;
+      col8 = (int)(unit - row * units_row);
+      step_row = step / units_row;
+      step_col8 = (int)(step - step_row * units_row);
+    }
+  }
+  __device__ void next() {
+    unit += step;
+    if (!FLAT) {
+      row += step_row;
+      col8 += step_col8;
+      if (col8 >= units_row) { col8 -= units_row; ++row; }
+    }
+  }
+  __device__ int64_t at(int64_t ld) const { return FLAT ? unit * 8 : row * ld + col8 * 8; }
+  __device__ int left(int features) const { return FLAT ? 8 : features - col8 * 8; }
+};
+// 8 elements as they lie in memory (16 or 32 bytes), loaded before they are converted
+template <bool F32>
+struct Raw8 {
+  uint4 w[F32 ? 2 : 1];
+  __device__ void load(const void* p, int64_t i) {
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * (F32 ? 4 : 2));
+    w[0] = src[0];
+    if (F32) w[1] = src[1];
+  }
+  __device__ void get(float* x) const {
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      x[j] = F32 ? __uint_as_float(r[j]) : __uint_as_float(j & 1 ? r[j / 2] & 0xffff0000u : r[j / 2] << 16);
+  }
+};
+
+__device__ __forceinline__ void a8_write_unit(const float* x, int8_t* q, uint8_t* qe, int64_t unit, bool live) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const uint32_t e = a8_scale_byte(top);
+  const float inv = a8_inverse(e);
+  if (live) {
+    reinterpret_cast<uint2*>(q)[unit] = make_uint2(a8_pack4(x[0], x[1], x[2], x[3], inv), a8_pack4(x[4], x[5], x[6], x[7], inv));
+    if ((threadIdx.x & 3) == 0) qe[unit / 4] = (uint8_t)e;
   }
 }
 
-// Y = act(v), or with dA: Y = dA * act'(v)
-template <typename T, int ACT, bool GRAD>
+// units: tokens * wide / 8. A checkpoint's rows follow one another without a gap, so a unit's number is its place in it.
+template <bool F32, bool FLAT>
 __global__ void __launch_bounds__(256)
-a8_expand_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ qe, int64_t wide, const T* dA, T* Y,
-                 int64_t tokens, int64_t features, int64_t ldda, int64_t ldy) {
-  const int lane = threadIdx.x & 31;
-  const int64_t per_row = wide / 32, total = tokens * per_row;
-  for (int64_t b = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); b < total; b += (int64_t)gridDim.x * 8) {
-    const int64_t t = b / per_row, c = (b - t * per_row) * 32 + lane;
-    if (c >= features) continue;
-    const float v = (float)q[t * wide + c] * a8_step(qe[b]);
-    Y[t * ldy + c] = cvt<T>(GRAD ? ld1(dA + t * ldda + c) * act_slope<ACT>(v) : act_value<ACT>(v));
+a8_compress_kernel(const void* __restrict__ X, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int64_t wide,
+                   int64_t units, int features, int64_t ldx, bool vec) {
+  A8Walk<FLAT> w(wide);
+  // whole warps leave together: the shuffles need them (units is a multiple of 4, not of 32)
+  while (__any_sync(0xffffffffu, w.unit < units)) {
+    const int64_t unit0 = w.unit;
+    if (FLAT) {
+      Raw8<F32> r[kA8Unroll];
+#pragma unroll
+      for (int u = 0; u < kA8Unroll; ++u) {
+        if (w.unit < units) r[u].load(X, w.unit * 8);
+        else r[u] = Raw8<F32>{};
+        w.next();
+      }
+#pragma unroll
+      for (int u = 0; u < kA8Unroll; ++u) {
+        float x[8];
+        r[u].get(x);
+        a8_write_unit(x, q, qe, unit0 + u * w.step, unit0 + u * w.step < units);
+      }
+    } else {
+      float x[kA8Unroll][8];
+#pragma unroll
+      for (int u = 0; u < kA8Unroll; ++u) {
+        load8(X, F32, w.at(ldx), vec, w.unit < units ? w.left(features) : 0, x[u]);
+        w.next();
+      }
+#pragma unroll
+      for (int u = 0; u < kA8Unroll; ++u) a8_write_unit(x[u], q, qe, unit0 + u * w.step, unit0 + u * w.step < units);
+    }
   }
 }
 
-unsigned grid_for(int64_t blocks32) {
-  const int64_t g = (blocks32 + 7) / 8;
-  return (unsigned)(g < 148 * 32 ? g : 148 * 32);
+// Y = act(v), or GRAD: Y = dA * act'(v). dA and Y may be the same matrix.
+template <bool F32, int ACT, bool GRAD, bool FLAT>
+__global__ void __launch_bounds__(256)
+a8_expand_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ qe, int64_t wide, const void* dA, void* Y,
+                 int64_t units, int features, int64_t ldda, int64_t ldy, bool vec) {
+  A8Walk<FLAT> w(wide);
+  while (w.unit < units) {
+    A8Walk<FLAT> o = w;
+    uint2 b[kA8Unroll];
+    uint32_t e[kA8Unroll];
+    Raw8<F32> raw[GRAD && FLAT ? kA8Unroll : 1];
+#pragma unroll
+    for (int u = 0; u < kA8Unroll; ++u) {
+      if (w.unit < units) {
+        b[u] = __ldcs(reinterpret_cast<const uint2*>(q) + w.unit);
+        e[u] = qe[w.unit / 4];
+        if (GRAD && FLAT) raw[u].load(dA, w.unit * 8);
+      }
+      w.next();
+    }
+#pragma unroll
+    for (int u = 0; u < kA8Unroll; ++u) {
+      const int n = o.unit < units ? o.left(features) : 0;
+      if (n > 0) {
+        float v[8], a[8];
+        if (GRAD && FLAT) raw[u].get(a);
+        if (GRAD && !FLAT) load8(dA, F32, o.at(ldda), vec, n, a);
+        a8_unpack4(b[u].x, a8_step(e[u]), v);
+        a8_unpack4(b[u].y, a8_step(e[u]), v + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = GRAD ? a[j] * act_slope<ACT>(v[j]) : act_value<ACT>(v[j]);
+        store8(Y, F32, o.at(ldy), vec, n, v);
+      }
+      o.next();
+    }
+  }
+}
+
+unsigned grid_for(int64_t units) {
+  const int64_t g = (units + 256 * kA8Unroll - 1) / (256 * kA8Unroll), most = 148 * 16;
+  return (unsigned)(g < most ? g : most);
+}
+bool vec_ok(const void* p, int64_t ld, int dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * (dtype == SC_DTYPE_BF16 ? 2 : 4)) % 16 == 0;
+}
+// one stretch of memory whose blocks of 32 are the checkpoint's (a single row of full blocks too)
+bool flat_ok(const void* p, int64_t ld, int64_t tokens, int64_t features) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && features % 32 == 0 && (ld == features || tokens == 1);
 }
 
 sc_status check(const void* act8, int dtype, int64_t tokens, int64_t features) {
@@ -61,20 +166,27 @@ sc_status check(const void* act8, int dtype, int64_t tokens, int64_t features) {
 }
 bool off(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == SC_DTYPE_BF16 ? 1 : 3)) != 0; }
 
-template <typename T, int ACT, bool GRAD>
+template <bool F32, int ACT, bool GRAD>
 void expand_one(const Act8View& v, const void* dA, void* Y, int64_t tokens, int64_t features, int64_t ldda, int64_t ldy,
                 cudaStream_t s) {
-  a8_expand_kernel<T, ACT, GRAD><<<grid_for(tokens * (v.wide / 32)), 256, 0, s>>>(
-      v.q, v.e, v.wide, static_cast<const T*>(dA), static_cast<T*>(Y), tokens, features, ldda, ldy);
+  const int dtype = F32 ? SC_DTYPE_FP32 : SC_DTYPE_BF16;
+  const int64_t units = tokens * (v.wide / 8);
+  const unsigned grid = grid_for(units);
+  if (flat_ok(Y, ldy, tokens, features) && (!GRAD || flat_ok(dA, ldda, tokens, features))) {
+    a8_expand_kernel<F32, ACT, GRAD, true><<<grid, 256, 0, s>>>(v.q, v.e, v.wide, dA, Y, units, (int)features, ldda, ldy, true);
+  } else {
+    const bool vec = vec_ok(Y, ldy, dtype) && (!GRAD || vec_ok(dA, ldda, dtype));
+    a8_expand_kernel<F32, ACT, GRAD, false><<<grid, 256, 0, s>>>(v.q, v.e, v.wide, dA, Y, units, (int)features, ldda, ldy, vec);
+  }
 }
-template <typename T, bool GRAD>
+template <bool F32, bool GRAD>
 void expand_act(const Act8View& v, int act, const void* dA, void* Y, int64_t tokens, int64_t features, int64_t ldda,
                 int64_t ldy, cudaStream_t s) {
   switch (act) {
-    case SC_ACT_RELU: expand_one<T, SC_ACT_RELU, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s); break;
-    case SC_ACT_GELU: expand_one<T, SC_ACT_GELU, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s); break;
-    case SC_ACT_SILU: expand_one<T, SC_ACT_SILU, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s); break;
-    default: expand_one<T, SC_ACT_NONE, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s);
+    case SC_ACT_RELU: expand_one<F32, SC_ACT_RELU, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s); break;
+    case SC_ACT_GELU: expand_one<F32, SC_ACT_GELU, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s); break;
+    case SC_ACT_SILU: expand_one<F32, SC_ACT_SILU, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s); break;
+    default: expand_one<F32, SC_ACT_NONE, GRAD>(v, dA, Y, tokens, features, ldda, ldy, s);
   }
 }
 
@@ -99,12 +211,18 @@ extern "C" sc_status sc_act8_compress(const void* X_dev, int dtype, void* act8_d
   if (!X_dev) return SC_ERR_INVALID_ARG;
   if (off(X_dev, dtype)) return SC_ERR_ALIGNMENT;
   const Act8View v = act8_view(act8_dev, tokens, features);
-  const unsigned grid = grid_for(tokens * (v.wide / 32));
+  const int64_t units = tokens * (v.wide / 8);
+  const unsigned grid = grid_for(units);
+  const bool vec = vec_ok(X_dev, ldx, dtype), flat = flat_ok(X_dev, ldx, tokens, features);
+  const int n = (int)features;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == SC_DTYPE_BF16)
-    a8_compress_kernel<bf16><<<grid, 256, 0, s>>>(static_cast<const bf16*>(X_dev), v.q, v.e, v.wide, tokens, features, ldx);
-  else
-    a8_compress_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float*>(X_dev), v.q, v.e, v.wide, tokens, features, ldx);
+  if (dtype == SC_DTYPE_BF16) {
+    if (flat) a8_compress_kernel<false, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
+    else a8_compress_kernel<false, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
+  } else {
+    if (flat) a8_compress_kernel<true, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
+    else a8_compress_kernel<true, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
+  }
   ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }
@@ -120,8 +238,8 @@ extern "C" sc_status sc_act8_expand(const void* act8_dev, int act, void* Y_dev, 
   if (off(Y_dev, dtype)) return SC_ERR_ALIGNMENT;
   const Act8View v = act8_view(const_cast<void*>(act8_dev), tokens, features);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == SC_DTYPE_BF16) expand_act<bf16, false>(v, act, nullptr, Y_dev, tokens, features, 0, ldy, s);
-  else expand_act<float, false>(v, act, nullptr, Y_dev, tokens, features, 0, ldy, s);
+  if (dtype == SC_DTYPE_BF16) expand_act<false, false>(v, act, nullptr, Y_dev, tokens, features, 0, ldy, s);
+  else expand_act<true, false>(v, act, nullptr, Y_dev, tokens, features, 0, ldy, s);
   ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }
@@ -137,8 +255,8 @@ extern "C" sc_status sc_act8_backward(const void* dA_dev, const void* act8_dev, 
   if (off(dA_dev, dtype) || off(dZ_dev, dtype)) return SC_ERR_ALIGNMENT;
   const Act8View v = act8_view(const_cast<void*>(act8_dev), tokens, features);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == SC_DTYPE_BF16) expand_act<bf16, true>(v, act, dA_dev, dZ_dev, tokens, features, ldda, lddz, s);
-  else expand_act<float, true>(v, act, dA_dev, dZ_dev, tokens, features, ldda, lddz, s);
+  if (dtype == SC_DTYPE_BF16) expand_act<false, true>(v, act, dA_dev, dZ_dev, tokens, features, ldda, lddz, s);
+  else expand_act<true, true>(v, act, dA_dev, dZ_dev, tokens, features, ldda, lddz, s);
   ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }

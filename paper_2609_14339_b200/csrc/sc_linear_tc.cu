@@ -55,74 +55,6 @@ __device__ __forceinline__ uint64_t lt_desc(uint32_t saddr, bool mn, int k16) {
 }
 
 // ---------------------------------------------------------------------------------------- epilogue, one row per thread
-__device__ __forceinline__ void load8(const void* p, int f32, int64_t i, bool vec, int n, float* r) {
-  if (vec && n >= 8) {
-    if (f32) {
-      const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-      const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i + 4);
-      r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w; r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
-    } else {
-      const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(p) + i);
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) { r[2 * j] = __uint_as_float(w[j] << 16); r[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      r[j] = j < n ? (f32 ? static_cast<const float*>(p)[i + j] : __bfloat162float(static_cast<const bf16*>(p)[i + j])) : 0.f;
-  }
-}
-__device__ __forceinline__ void store8(void* p, int f32, int64_t i, bool vec, int n, const float* v) {
-  if (vec && n >= 8) {
-    if (f32) {
-      float* o = static_cast<float*>(p) + i;
-      *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-        w[j] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-      *reinterpret_cast<uint4*>(static_cast<bf16*>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) {
-        if (f32) static_cast<float*>(p)[i + j] = v[j];
-        else static_cast<bf16*>(p)[i + j] = __float2bfloat16_rn(v[j]);
-      }
-  }
-}
-
-template <int N_, typename F>
-__device__ __forceinline__ void each(float* v, F f) {
-#pragma unroll
-  for (int j = 0; j < N_; ++j) v[j] = f(v[j]);
-}
-// the activation is uniform over the launch: one branch per block of values
-template <int N_>
-__device__ __forceinline__ void act_values(int act, float* v) {
-  switch (act) {
-    case SC_ACT_RELU: each<N_>(v, [](float z) { return act_value<SC_ACT_RELU>(z); }); break;
-    case SC_ACT_GELU: each<N_>(v, [](float z) { return act_value<SC_ACT_GELU>(z); }); break;
-    case SC_ACT_SILU: each<N_>(v, [](float z) { return act_value<SC_ACT_SILU>(z); }); break;
-    default: break;
-  }
-}
-template <int N_>
-__device__ __forceinline__ void act_slopes(int act, float* v) {
-  switch (act) {
-    case SC_ACT_RELU: each<N_>(v, [](float z) { return act_slope<SC_ACT_RELU>(z); }); break;
-    case SC_ACT_GELU: each<N_>(v, [](float z) { return act_slope<SC_ACT_GELU>(z); }); break;
-    case SC_ACT_SILU: each<N_>(v, [](float z) { return act_slope<SC_ACT_SILU>(z); }); break;
-    default: each<N_>(v, [](float) { return 1.f; });
-  }
-}
-
 // 32 neighbouring columns (from a multiple of 32) of one row: v holds the sums
 template <int KIND>
 __device__ __forceinline__ void epilogue_row32(const LinEpilogue& e, const LtShape& sh, const float* aux, float* v,

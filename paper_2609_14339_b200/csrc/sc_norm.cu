@@ -5,126 +5,435 @@
 namespace sc {
 namespace {
 
-constexpr int kNormThreads = 256;
-constexpr int kNormSlices = 296;       // row slices of the column sums at most (fixed-order two-stage reduction)
+// Rows of up to kRowMax columns live in registers from their one read on: a block owns a row at a time, a thread 8 (or 4)
+// of its columns, and the next row of the block is already on its way while this one is reduced and written.
+constexpr int kRowMax = 8192;          // 1024 threads x 8 columns
+constexpr int kWideThreads = 256;      // wider rows: re-read per pass instead
+constexpr int kJoinCols = 32, kJoinParts = 32;
 
-template <typename T>
-__device__ __forceinline__ float ld1(const T* p);
-template <>
-__device__ __forceinline__ float ld1<float>(const float* p) { return *p; }
-template <>
-__device__ __forceinline__ float ld1<bf16>(const bf16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void st1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void st1(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-// sum over the block, the same value in every thread (fixed order: lanes, then warps)
-__device__ __forceinline__ float block_sum(float v, float* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  const int warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[warp] = v;
-  __syncthreads();
-  float s = 0.f;
-  for (int w = 0; w < n_warps; ++w) s += red[w];
-  return s;
+constexpr int blocks_per_sm(int threads, int threads_per_sm) {
+  return threads_per_sm / threads < 1 ? 1 : threads_per_sm / threads < 16 ? threads_per_sm / threads : 16;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kNormThreads)
-norm_forward_kernel(const T* __restrict__ X, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
-                    T* __restrict__ Y, float* __restrict__ stats, int8_t* __restrict__ q, uint8_t* __restrict__ qe,
-                    int64_t wide, int64_t rows, int cols, int64_t ldx, int64_t ldy) {
-  __shared__ float red[kNormThreads / 32];
+template <bool F32>
+__device__ __forceinline__ float ld1(const void* p, int64_t i) {
+  return F32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const bf16*>(p)[i]);
+}
+template <bool F32>
+__device__ __forceinline__ void st1(void* p, int64_t i, float v) {
+  if (F32) static_cast<float*>(p)[i] = v;
+  else static_cast<bf16*>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// s / n by the reciprocal, corrected once: a row of equal values has exactly that mean (and n exactly 0: with an rstd of
+// 1 / sqrt(eps) a last-bit error in the mean would show)
+__device__ __forceinline__ float mean_of(float s, float n, float inv_n) {
+  const float m = s * inv_n;
+  return fmaf(fmaf(-m, n, s), inv_n, m);
+}
+
+// Sums of two values over the block, the same in every thread; the order (lanes, then warps) is fixed. The first exchange
+// leaves one value with each half of the warp, which halves the shuffles. `red` holds two sets of slots, used in turn, so
+// that one barrier per call is enough.
+__device__ __forceinline__ void block_sums(float& a, float& b, float (*red)[2][32], int& turn) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
+  const bool high = lane & 16;
+  float v = high ? b : a;
+  v += __shfl_xor_sync(0xffffffffu, high ? a : b, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (n_warps > 1) {
+    if ((lane & 15) == 0) red[turn][lane >> 4][warp] = v;
+    __syncthreads();
+    const float* mine = red[turn][lane >> 4];
+    const int k = lane & 15;
+    v = (k < n_warps ? mine[k] : 0.f) + (k + 16 < n_warps ? mine[k + 16] : 0.f);
+    turn ^= 1;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  a = __shfl_sync(0xffffffffu, v, 0);
+  b = __shfl_sync(0xffffffffu, v, 16);
+}
+
+// A thread's EPT columns of one row, as they lie in memory. VEC: EPT neighbours from thread * EPT on in 16-byte accesses
+// (the number of columns is a multiple of EPT, so a thread's columns are all inside the row or all outside); otherwise
+// every blockDim-th column, one at a time (any stride, alignment and width, still coalesced). Outside the row: zeros.
+template <bool F32, int EPT, bool VEC>
+struct Piece {
+  static constexpr int kWords = EPT * (F32 ? 4 : 2) / 4;
+  uint32_t w[VEC ? kWords : EPT];
+  __device__ static int col(int i) { return VEC ? (int)threadIdx.x * EPT + i : (int)threadIdx.x + i * (int)blockDim.x; }
+  __device__ static bool in(int i, int cols) { return col(VEC ? 0 : i) < cols; }
+  __device__ void load(const void* p, int64_t at, int cols) {
+    if (VEC) {
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + (at + col(0)) * (F32 ? 4 : 2));
+      const bool live = in(0, cols);
+#pragma unroll
+      for (int k = 0; k < kWords / 4; ++k) {
+        const uint4 u = live ? src[k] : make_uint4(0u, 0u, 0u, 0u);
+        w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) w[i] = in(i, cols) ? __float_as_uint(ld1<F32>(p, at + col(i))) : 0u;
+    }
+  }
+  __device__ float get(int i) const {
+    if (!VEC || F32) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+};
+template <bool F32, int EPT, bool VEC>
+__device__ __forceinline__ void store_piece(void* p, int64_t at, int cols, const float* v) {
+  typedef Piece<F32, EPT, VEC> P;
+  if (VEC) {
+    if (P::in(0, cols)) {
+      if (EPT >= 8) {
+#pragma unroll
+        for (int i = 0; i < EPT; i += 8) store8(p, F32, at + P::col(i), true, 8, v + i);
+      } else {
+        *reinterpret_cast<float4*>(static_cast<float*>(p) + at + P::col(0)) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPT; ++i)
+      if (P::in(i, cols)) st1<F32>(p, at + P::col(i), v[i]);
+  }
+}
+
+// EPT fp32 parameters of this thread's columns; 0 outside the row
+template <int EPT, bool VEC>
+__device__ __forceinline__ void load_params(const float* p, int cols, float missing, float* v) {
+  typedef Piece<true, EPT, VEC> P;
+  if (p && VEC && P::in(0, cols)) {
+#pragma unroll
+    for (int i = 0; i < EPT; i += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4*>(p + P::col(i)));
+      v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) v[i] = P::in(i, cols) ? (p ? __ldg(p + P::col(i)) : missing) : 0.f;
+  }
+}
+
+// The parameters of a thread's columns in shared memory, four at a time and lane after lane: read again for every row
+// instead of held in registers, which the rows in flight need.
+template <int EPT, int THREADS>
+struct Params {
+  float4 v[EPT / 4][THREADS];
+  template <bool VEC>
+  __device__ void fill(const float* p, int cols, float missing) {
+    float w[EPT];
+    load_params<EPT, VEC>(p, cols, missing, w);
+#pragma unroll
+    for (int k = 0; k < EPT / 4; ++k) v[k][threadIdx.x] = make_float4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+  }
+  __device__ float4 get(int k) const { return v[k][threadIdx.x]; }
+};
+
+// A block takes ROWS neighbouring rows at a time, which share barriers, shuffles and parameters; the next ones are on their
+// way meanwhile. With 8 columns a thread two rows are what makes the shared work small; with 16 one row's is, and a second
+// would not fit the 64 registers that let two blocks of 512 share an SM.
+template <bool F32, int EPT, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS, blocks_per_sm(THREADS, 1024))
+norm_forward_kernel(const void* X, const float* __restrict__ weight, const float* __restrict__ bias, float eps, void* Y,
+                    float* __restrict__ stats, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int64_t wide, int64_t rows,
+                    int cols, int64_t ldx, int64_t ldy) {
+  extern __shared__ float4 param_smem[];
+  __shared__ float red[2][2][32];
+  typedef Piece<F32, EPT, VEC> P;
+  typedef Params<EPT, THREADS> W;
+  constexpr int ROWS = EPT == 16 ? 1 : 2;
+  W* pw = reinterpret_cast<W*>(param_smem);
+  W* pb = pw + 1;
+  pw->template fill<VEC>(weight, cols, 1.f);
+  pb->template fill<VEC>(bias, cols, 0.f);
+  int turn = 0;
+  const float n = (float)cols, inv_n = 1.f / n;
+  P ahead[ROWS];
+  const int64_t groups = (rows + ROWS - 1) / ROWS;
+  const auto fetch = [&](int64_t g) {
+    if (g < groups) {
+#pragma unroll
+      for (int h = 0; h < ROWS; ++h) {
+        if (ROWS * g + h < rows) ahead[h].load(X, (ROWS * g + h) * ldx, cols);
+        else ahead[h] = P{};
+      }
+    }
+  };
+  fetch(blockIdx.x);
+  for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
+    P x[ROWS];
+#pragma unroll
+    for (int h = 0; h < ROWS; ++h) x[h] = ahead[h];
+    fetch(g + gridDim.x);
+    float s[2] = {0.f, 0.f}, mean[2], rstd[2];
+#pragma unroll
+    for (int h = 0; h < ROWS; ++h)
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) s[h] += x[h].get(i);
+    block_sums(s[0], s[1], red, turn);
+#pragma unroll
+    for (int h = 0; h < ROWS; ++h) {
+      mean[h] = mean_of(s[h], n, inv_n);
+      s[h] = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        const float d = VEC || P::in(i, cols) ? x[h].get(i) - mean[h] : 0.f;
+        s[h] = fmaf(d, d, s[h]);
+      }
+      if (VEC && !P::in(0, cols)) s[h] = 0.f;
+    }
+    block_sums(s[0], s[1], red, turn);
+#pragma unroll
+    for (int h = 0; h < ROWS; ++h) {
+      const int64_t r = ROWS * g + h;
+      rstd[h] = rsqrtf(s[h] * inv_n + eps);
+      if (ROWS > 1 && r >= rows) continue;
+      if (stats && threadIdx.x == 0) { stats[r] = mean[h]; stats[rows + r] = rstd[h]; }
+      float y[EPT];            // outside the row: 0 (weight and bias are 0 there)
+#pragma unroll
+      for (int k = 0; k < EPT / 4; ++k) {
+        const float4 w = pw->get(k), b = pb->get(k);
+        const float wv[4] = {w.x, w.y, w.z, w.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[4 * k + i] = fmaf((x[h].get(4 * k + i) - mean[h]) * rstd[h], wv[i], bv[i]);
+      }
+      if (q) {                 // blocks of 32 columns: 32 / EPT neighbouring threads, or the 32 lanes of a warp
+        if (VEC) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int i = 0; i < EPT; ++i) top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);
+#pragma unroll
+          for (int o = 1; o < 32 / EPT; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const uint32_t e = a8_scale_byte(top);
+          const float inv = a8_inverse(e);
+          const int c = P::col(0);
+          if (c < wide) {
+#pragma unroll
+            for (int i = 0; i < EPT; i += 4)
+              *reinterpret_cast<uint32_t*>(q + r * wide + c + i) = a8_pack4(y[i], y[i + 1], y[i + 2], y[i + 3], inv);
+            if (threadIdx.x % (32 / EPT) == 0) qe[r * (wide / 32) + c / 32] = (uint8_t)e;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < EPT; ++i) {
+            const uint32_t e = a8_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(y[i]) & 0x7fffffffu));
+            const float inv = a8_inverse(e);
+            const int c = P::col(i);
+            if (c < wide) {
+              q[r * wide + c] = (int8_t)(inv == 0.f ? 0u : a8_round(y[i], inv) & 255u);
+              if ((threadIdx.x & 31) == 0) qe[r * (wide / 32) + c / 32] = (uint8_t)e;
+            }
+          }
+        }
+      }
+      store_piece<F32, EPT, VEC>(Y, r * ldy, cols, y);
+    }
+  }
+}
+
+// dX of the block's rows, and the block's share of the column sums, kept in registers over all of them.
+template <bool F32, int EPT, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS, blocks_per_sm(THREADS, EPT == 16 ? 512 : 1024))
+norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ weight, const float* __restrict__ stats,
+                     const void* R, void* dX, float* __restrict__ part, int64_t rows, int cols, int64_t lddy, int64_t ldx,
+                     int64_t ldr, int64_t lddx) {
+  __shared__ float red[2][2][32];
+  __shared__ Params<EPT, THREADS> pw;
+  typedef Piece<F32, EPT, VEC> P;
+  constexpr bool AHEAD = VEC && !(F32 && EPT == 8);      // the next row on its way, as far as the registers go
+  constexpr bool RES_AHEAD = AHEAD && !F32;
+  int turn = 0;
+  const float inv_n = 1.f / (float)cols;
+  pw.template fill<VEC>(weight, cols, 1.f);
+  float sw[EPT], sb[EPT];
+#pragma unroll
+  for (int i = 0; i < EPT; ++i) sw[i] = sb[i] = 0.f;
+  P nx, ny, nr;
+  float n_mean = 0.f, n_rstd = 0.f;
+  const auto fetch = [&](int64_t r) {
+    nx.load(X, r * ldx, cols);
+    ny.load(dY, r * lddy, cols);
+    if (RES_AHEAD && R) nr.load(R, r * ldr, cols);
+    n_mean = stats[r];
+    n_rstd = stats[rows + r];
+  };
+  if (AHEAD) fetch(blockIdx.x);
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const T* x = X + r * ldx;
-    float s = 0.f;
-    for (int c = threadIdx.x; c < cols; c += kNormThreads) s += ld1(x + c);
-    const float mean = block_sum(s, red) / (float)cols;
+    if (!AHEAD) fetch(r);
+    const P x = nx, dy = ny;
+    const float mean = n_mean, rstd = n_rstd;
+    P res = nr;
+    if (!RES_AHEAD && R) res.load(R, r * ldr, cols);
+    if (AHEAD && r + gridDim.x < rows) fetch(r + gridDim.x);
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int k = 0; k < EPT / 4; ++k) {
+      const float4 w4 = pw.get(k);
+      const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * k + j;
+        const float d = dy.get(i), n = (x.get(i) - mean) * rstd, g = d * w[j];        // outside the row d = 0
+        s0 += g;
+        s1 = fmaf(g, n, s1);
+        sw[i] = fmaf(d, n, sw[i]);
+        sb[i] += d;
+      }
+    }
+    block_sums(s0, s1, red, turn);
+    const float m0 = s0 * inv_n, m1 = s1 * inv_n;
+    float v[EPT];
+#pragma unroll
+    for (int k = 0; k < EPT / 4; ++k) {
+      const float4 w4 = pw.get(k);
+      const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * k + j;
+        const float n = (x.get(i) - mean) * rstd, t = fmaf(-n, m1, fmaf(dy.get(i), w[j], -m0));
+        v[i] = fmaf(t, rstd, R ? res.get(i) : 0.f);
+      }
+    }
+    store_piece<F32, EPT, VEC>(dX, r * lddx, cols, v);
+  }
+  if (part) {
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {
+      if (P::in(i, cols)) {
+        part[((size_t)blockIdx.x * 2 + 0) * cols + P::col(i)] = sw[i];
+        part[((size_t)blockIdx.x * 2 + 1) * cols + P::col(i)] = sb[i];
+      }
+    }
+  }
+}
+
+// ---- rows of more than kRowMax columns: one block per row, three reads (the second and third from L2) -------------------
+template <bool F32>
+__global__ void __launch_bounds__(kWideThreads)
+norm_forward_wide_kernel(const void* X, const float* __restrict__ weight, const float* __restrict__ bias, float eps, void* Y,
+                         float* __restrict__ stats, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int64_t wide,
+                         int64_t rows, int cols, int64_t ldx, int64_t ldy) {
+  __shared__ float red[2][2][32];
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const int64_t x = r * ldx;
+    float s = 0.f, none = 0.f;
+    for (int c = threadIdx.x; c < cols; c += kWideThreads) s += ld1<F32>(X, x + c);
+    block_sums(s, none, red, turn);
+    const float mean = s / (float)cols;
     s = 0.f;
-    for (int c = threadIdx.x; c < cols; c += kNormThreads) { const float d = ld1(x + c) - mean; s += d * d; }
-    const float rstd = 1.f / sqrtf(block_sum(s, red) / (float)cols + eps);
+    for (int c = threadIdx.x; c < cols; c += kWideThreads) { const float d = ld1<F32>(X, x + c) - mean; s += d * d; }
+    block_sums(s, none, red, turn);
+    const float rstd = rsqrtf(s / (float)cols + eps);
     if (stats && threadIdx.x == 0) { stats[r] = mean; stats[rows + r] = rstd; }
-    // the padding of the last block of 32 is written too, as zeros
-    const int width = q ? (int)wide : cols;
-    for (int c = threadIdx.x; c < (width + 31) / 32 * 32; c += kNormThreads) {
+    const int width = (q ? (int)wide : cols) + 31 & ~31;      // whole warps: the padding of the last block of 32 too
+    for (int c = threadIdx.x; c < width; c += kWideThreads) {
       float y = 0.f;
       if (c < cols) {
-        y = (ld1(x + c) - mean) * rstd;
+        y = (ld1<F32>(X, x + c) - mean) * rstd;
         if (weight) y *= weight[c];
         if (bias) y += bias[c];
       }
-      if (q) {       // 32 neighbouring columns are the 32 lanes of a warp
-        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(y) & 0x7fffffffu);
-        const uint32_t e = a8_scale_byte(top);
+      if (q) {
+        const uint32_t e = a8_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(y) & 0x7fffffffu));
         const float inv = a8_inverse(e);
         q[r * wide + c] = (int8_t)(inv == 0.f ? 0u : a8_round(y, inv) & 255u);
         if ((threadIdx.x & 31) == 0) qe[r * (wide / 32) + c / 32] = (uint8_t)e;
       }
-      if (c < cols) st1(Y + r * ldy + c, y);
+      if (c < cols) st1<F32>(Y, r * ldy + c, y);
     }
-    __syncthreads();
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kNormThreads)
-norm_backward_kernel(const T* dY, const T* __restrict__ X, const float* __restrict__ weight,
-                     const float* __restrict__ stats, const T* R, T* dX, int64_t rows, int cols, int64_t lddy,
-                     int64_t ldx, int64_t ldr, int64_t lddx) {
-  __shared__ float red[kNormThreads / 32];
+template <bool F32>
+__global__ void __launch_bounds__(kWideThreads)
+norm_backward_wide_kernel(const void* dY, const void* X, const float* __restrict__ weight, const float* __restrict__ stats,
+                          const void* R, void* dX, int64_t rows, int cols, int64_t lddy, int64_t ldx, int64_t ldr,
+                          int64_t lddx) {
+  __shared__ float red[2][2][32];
+  int turn = 0;
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const T *x = X + r * ldx, *dy = dY + r * lddy;
     const float mean = stats[r], rstd = stats[rows + r];
-    float s0 = 0.f, s1 = 0.f;
-    for (int c = threadIdx.x; c < cols; c += kNormThreads) {
-      const float g = ld1(dy + c) * (weight ? weight[c] : 1.f);
-      s0 += g;
-      s1 += g * (ld1(x + c) - mean) * rstd;
+    float s[2] = {0.f, 0.f};
+    for (int c = threadIdx.x; c < cols; c += kWideThreads) {
+      const float g = ld1<F32>(dY, r * lddy + c) * (weight ? weight[c] : 1.f);
+      s[0] += g;
+      s[1] += g * (ld1<F32>(X, r * ldx + c) - mean) * rstd;
     }
-    const float m0 = block_sum(s0, red) / (float)cols, m1 = block_sum(s1, red) / (float)cols;
-    for (int c = threadIdx.x; c < cols; c += kNormThreads) {
-      const float g = ld1(dy + c) * (weight ? weight[c] : 1.f);
-      float v = rstd * (g - m0 - (ld1(x + c) - mean) * rstd * m1);
-      if (R) v += ld1(R + r * ldr + c);
-      st1(dX + r * lddx + c, v);
+    block_sums(s[0], s[1], red, turn);
+    const float m0 = s[0] / (float)cols, m1 = s[1] / (float)cols;
+    for (int c = threadIdx.x; c < cols; c += kWideThreads) {
+      const float g = ld1<F32>(dY, r * lddy + c) * (weight ? weight[c] : 1.f);
+      float v = rstd * (g - m0 - (ld1<F32>(X, r * ldx + c) - mean) * rstd * m1);
+      if (R) v += ld1<F32>(R, r * ldr + c);
+      st1<F32>(dX, r * lddx + c, v);
     }
-    __syncthreads();
   }
 }
 
 // column sums of dY n and dY over one slice of the rows
-template <typename T>
+template <bool F32>
 __global__ void __launch_bounds__(128)
-norm_columns_kernel(const T* __restrict__ dY, const T* __restrict__ X, const float* __restrict__ stats,
+norm_columns_kernel(const void* __restrict__ dY, const void* __restrict__ X, const float* __restrict__ stats,
                     float* __restrict__ part, int64_t rows, int cols, int64_t lddy, int64_t ldx) {
   const int c = blockIdx.x * 128 + threadIdx.x;
   if (c >= cols) return;
   float sw = 0.f, sb = 0.f;
   for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
-    const float d = ld1(dY + r * lddy + c);
-    sw += d * ((ld1(X + r * ldx + c) - stats[r]) * stats[rows + r]);
+    const float d = ld1<F32>(dY, r * lddy + c);
+    sw += d * ((ld1<F32>(X, r * ldx + c) - stats[r]) * stats[rows + r]);
     sb += d;
   }
   part[((size_t)blockIdx.y * 2 + 0) * cols + c] = sw;
   part[((size_t)blockIdx.y * 2 + 1) * cols + c] = sb;
 }
 
-__global__ void __launch_bounds__(128)
+// the slices' sums, joined in a fixed order: 32 threads per column take every 32nd slice, then the 32 are added in turn
+__global__ void __launch_bounds__(kJoinCols * kJoinParts)
 norm_columns_join_kernel(const float* __restrict__ part, int slices, float* __restrict__ dweight,
                          float* __restrict__ dbias, int cols) {
-  const int c = blockIdx.x * 128 + threadIdx.x;
-  if (c >= cols) return;
+  __shared__ float red[2][kJoinParts][kJoinCols + 1];
+  const int lane = threadIdx.x % kJoinCols, y = threadIdx.x / kJoinCols, c = blockIdx.x * kJoinCols + lane;
   float sw = 0.f, sb = 0.f;
-  for (int s = 0; s < slices; ++s) {
-    sw += part[((size_t)s * 2 + 0) * cols + c];
-    sb += part[((size_t)s * 2 + 1) * cols + c];
+  if (c < cols) {
+#pragma unroll 4
+    for (int s = y; s < slices; s += kJoinParts) {
+      sw += part[((size_t)s * 2 + 0) * cols + c];
+      sb += part[((size_t)s * 2 + 1) * cols + c];
+    }
   }
-  if (dweight) dweight[c] = sw;
-  if (dbias) dbias[c] = sb;
+  red[0][y][lane] = sw;
+  red[1][y][lane] = sb;
+  __syncthreads();
+  if (y < 2 && c < cols) {
+    float s = 0.f;
+    for (int k = 0; k < kJoinParts; ++k) s += red[y][k][lane];
+    float* out = y == 0 ? dweight : dbias;
+    if (out) out[c] = s;
+  }
 }
 
-int norm_slices(int64_t rows) { return rows < kNormSlices ? (int)(rows > 0 ? rows : 1) : kNormSlices; }
+// Threads of a row's block, a power of two of them so that few kernels are built.
+int row_threads(int64_t cols, int ept) {
+  int t = 32;
+  while ((int64_t)t * ept < cols) t *= 2;
+  return t;
+}
+
+// Slices of the column sums: one per block of the backward kernel. All the blocks that are resident at once, but at
+// least four rows each: a block's share of the sums is two rows' worth of fp32 to write and to read again.
+constexpr int kNormSms = 148;
+int norm_slices(int64_t rows, int64_t cols) {
+  const int64_t most = cols <= kRowMax ? (int64_t)kNormSms * (1024 / row_threads(cols, 8) < 16 ? 1024 / row_threads(cols, 8) : 16)
+                                       : 2 * kNormSms;
+  const int64_t want = (rows + 3) / 4;
+  return (int)(want < 1 ? 1 : want < most ? want : most);
+}
 
 sc_status check_rows(int64_t rows, int64_t cols) {
   if (rows < 0 || cols <= 0) return SC_ERR_SHAPE;
@@ -134,44 +443,137 @@ sc_status check_rows(int64_t rows, int64_t cols) {
 int elem(int dtype) { return dtype == SC_DTYPE_BF16 ? 2 : 4; }
 bool off(const void* p, int n) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(n - 1)) != 0; }
 
-template <typename T>
-sc_status forward(const void* X, const void* w, const void* b, float eps, void* Y, void* stats, void* act8, int64_t rows,
-                  int64_t cols, int64_t ldx, int64_t ldy, cudaStream_t s) {
-  Act8View v{};
-  if (act8) v = act8_view(act8, rows, cols);
-  const unsigned grid = (unsigned)(rows < (1 << 20) ? rows : (1 << 20));
-  norm_forward_kernel<T><<<grid, kNormThreads, 0, s>>>(static_cast<const T*>(X), static_cast<const float*>(w),
-                                                       static_cast<const float*>(b), eps, static_cast<T*>(Y),
-                                                       static_cast<float*>(stats), v.q, v.e, v.wide, rows, (int)cols, ldx,
-                                                       ldy);
+bool vec_row(const void* p, int64_t ld, int dtype) {
+  return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * elem(dtype)) % 16 == 0);
+}
+
+struct Forward {
+  const void* X;
+  const float *w, *b;
+  float eps;
+  void* Y;
+  float* stats;
+  Act8View a8;
+  int64_t rows, cols, ldx, ldy;
+};
+template <bool F32, int EPT, bool VEC, int THREADS>
+void forward_launch(const Forward& f, cudaStream_t s) {
+  const int smem = 2 * (int)sizeof(Params<EPT, THREADS>);
+  if (smem > 40 * 1024)
+    cudaFuncSetAttribute(norm_forward_kernel<F32, EPT, VEC, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int64_t most = (int64_t)kNormSms * blocks_per_sm(THREADS, 1024), groups = EPT == 16 ? f.rows : (f.rows + 1) / 2;
+  norm_forward_kernel<F32, EPT, VEC, THREADS><<<(unsigned)(groups < most ? groups : most), THREADS, smem, s>>>(
+      f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e, f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
+}
+struct Backward {
+  const void *dY, *X;
+  const float *w, *stats;
+  const void* R;
+  void* dX;
+  float* part;
+  int slices;
+  int64_t rows, cols, lddy, ldx, ldr, lddx;
+};
+template <bool F32, int EPT, bool VEC, int THREADS>
+void backward_launch(const Backward& f, cudaStream_t s) {
+  norm_backward_kernel<F32, EPT, VEC, THREADS><<<(unsigned)f.slices, THREADS, 0, s>>>(
+      f.dY, f.X, f.w, f.stats, f.R, f.dX, f.part, f.rows, (int)f.cols, f.lddy, f.ldx, f.ldr, f.lddx);
+}
+
+// one of the built block sizes for the row's width
+template <bool F32, int EPT, bool VEC, typename F>
+void by_threads(int threads, const F& f, cudaStream_t s) {
+  switch (threads) {
+    case 32: f.template go<F32, EPT, VEC, 32>(s); break;
+    case 64: f.template go<F32, EPT, VEC, 64>(s); break;
+    case 128: f.template go<F32, EPT, VEC, 128>(s); break;
+    case 256: f.template go<F32, EPT, VEC, 256>(s); break;
+    case 512: f.template go<F32, EPT, VEC, 512>(s); break;
+    default: f.template go<F32, EPT, VEC, EPT == 16 ? 512 : 1024>(s);       // 16 columns: 512 threads are a whole row
+  }
+}
+struct GoForward {
+  const Forward& f;
+  template <bool F32, int EPT, bool VEC, int THREADS>
+  void go(cudaStream_t s) const { forward_launch<F32, EPT, VEC, THREADS>(f, s); }
+};
+struct GoBackward {
+  const Backward& f;
+  template <bool F32, int EPT, bool VEC, int THREADS>
+  void go(cudaStream_t s) const { backward_launch<F32, EPT, VEC, THREADS>(f, s); }
+};
+
+// Columns per thread. The shuffles, barriers and addresses of a row cost the same for 8 columns as for 16, so bf16 rows
+// take 16 where the width allows it (one row's pieces are then 32 bytes a thread); fp32 rows 8, and the backward kernel 4
+// up to 4096 columns (three pieces of a row and the column sums have to fit in registers).
+template <bool F32>
+void forward_rows(const Forward& f, bool vec, cudaStream_t s) {
+  const GoForward go{f};
+  if (!F32 && vec && f.cols % 16 == 0) by_threads<F32, F32 ? 8 : 16, true>(row_threads(f.cols, 16), go, s);
+  else if (vec && f.cols % 8 == 0) by_threads<F32, 8, true>(row_threads(f.cols, 8), go, s);
+  else by_threads<F32, 8, false>(row_threads(f.cols, 8), go, s);
+}
+template <bool F32>
+void backward_rows(const Backward& f, bool vec, cudaStream_t s) {
+  const GoBackward go{f};
+  if (F32 && f.cols <= 4096) {
+    if (vec && f.cols % 4 == 0) by_threads<F32, F32 ? 4 : 8, true>(row_threads(f.cols, 4), go, s);
+    else by_threads<F32, F32 ? 4 : 8, false>(row_threads(f.cols, 4), go, s);
+  } else if (!F32 && vec && f.cols % 16 == 0) {
+    by_threads<F32, F32 ? 8 : 16, true>(row_threads(f.cols, 16), go, s);
+  } else {
+    if (vec && f.cols % 8 == 0) by_threads<F32, 8, true>(row_threads(f.cols, 8), go, s);
+    else by_threads<F32, 8, false>(row_threads(f.cols, 8), go, s);
+  }
+}
+
+sc_status forward(const Forward& f, int dtype, cudaStream_t s) {
+  if (f.cols <= kRowMax) {
+    const bool vec = vec_row(f.X, f.ldx, dtype) && vec_row(f.Y, f.ldy, dtype) && vec_row(f.w, 4, SC_DTYPE_FP32) &&
+                     vec_row(f.b, 4, SC_DTYPE_FP32);
+    if (dtype == SC_DTYPE_BF16) forward_rows<false>(f, vec, s);
+    else forward_rows<true>(f, vec, s);
+  } else {
+    const unsigned grid = (unsigned)(f.rows < (1 << 20) ? f.rows : (1 << 20));
+    if (dtype == SC_DTYPE_BF16)
+      norm_forward_wide_kernel<false><<<grid, kWideThreads, 0, s>>>(f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e,
+                                                                    f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
+    else
+      norm_forward_wide_kernel<true><<<grid, kWideThreads, 0, s>>>(f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e,
+                                                                   f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
+  }
   ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }
 
-template <typename T>
-sc_status backward(const void* dY, const void* X, const void* w, const void* stats, const void* R, void* dX, void* dw,
-                   void* db, int64_t rows, int64_t cols, int64_t lddy, int64_t ldx, int64_t ldr, int64_t lddx, float* part,
-                   cudaStream_t s) {
-  const unsigned blocks = (unsigned)((cols + 127) / 128);
-  int slices = 0;
-  if (rows > 0 && (dw || db)) {       // before dX is written: dX may be dY
-    slices = norm_slices(rows);
-    norm_columns_kernel<T><<<dim3(blocks, slices), 128, 0, s>>>(static_cast<const T*>(dY), static_cast<const T*>(X),
-                                                                static_cast<const float*>(stats), part, rows, (int)cols,
-                                                                lddy, ldx);
+sc_status backward(Backward f, int dtype, float* dw, float* db, cudaStream_t s) {
+  const bool sums = dw || db;
+  float* part = f.part;
+  f.slices = norm_slices(f.rows, f.cols);
+  if (!sums) f.part = nullptr;
+  if (f.rows > 0 && f.cols <= kRowMax) {
+    const bool vec = vec_row(f.X, f.ldx, dtype) && vec_row(f.dY, f.lddy, dtype) && vec_row(f.R, f.ldr, dtype) &&
+                     vec_row(f.dX, f.lddx, dtype) && vec_row(f.w, 4, SC_DTYPE_FP32);
+    if (dtype == SC_DTYPE_BF16) backward_rows<false>(f, vec, s);
+    else backward_rows<true>(f, vec, s);
     ++g_kernel_launches;
+  } else if (f.rows > 0) {
+    const unsigned grid = (unsigned)(f.rows < (1 << 20) ? f.rows : (1 << 20));
+    const dim3 cgrid((unsigned)((f.cols + 127) / 128), (unsigned)f.slices);
+    if (dtype == SC_DTYPE_BF16) {          // the column sums before dX is written: dX may be dY
+      if (sums) norm_columns_kernel<false><<<cgrid, 128, 0, s>>>(f.dY, f.X, f.stats, part, f.rows, (int)f.cols, f.lddy, f.ldx);
+      norm_backward_wide_kernel<false><<<grid, kWideThreads, 0, s>>>(f.dY, f.X, f.w, f.stats, f.R, f.dX, f.rows, (int)f.cols,
+                                                                     f.lddy, f.ldx, f.ldr, f.lddx);
+    } else {
+      if (sums) norm_columns_kernel<true><<<cgrid, 128, 0, s>>>(f.dY, f.X, f.stats, part, f.rows, (int)f.cols, f.lddy, f.ldx);
+      norm_backward_wide_kernel<true><<<grid, kWideThreads, 0, s>>>(f.dY, f.X, f.w, f.stats, f.R, f.dX, f.rows, (int)f.cols,
+                                                                    f.lddy, f.ldx, f.ldr, f.lddx);
+    }
+    g_kernel_launches += sums ? 2 : 1;
   }
-  if (dw || db) {
-    norm_columns_join_kernel<<<blocks, 128, 0, s>>>(part, slices, static_cast<float*>(dw), static_cast<float*>(db),
-                                                    (int)cols);
-    ++g_kernel_launches;
-  }
-  if (rows > 0) {
-    const unsigned grid = (unsigned)(rows < (1 << 20) ? rows : (1 << 20));
-    norm_backward_kernel<T><<<grid, kNormThreads, 0, s>>>(static_cast<const T*>(dY), static_cast<const T*>(X),
-                                                          static_cast<const float*>(w), static_cast<const float*>(stats),
-                                                          static_cast<const T*>(R), static_cast<T*>(dX), rows, (int)cols,
-                                                          lddy, ldx, ldr, lddx);
+  if (sums) {
+    norm_columns_join_kernel<<<(unsigned)((f.cols + kJoinCols - 1) / kJoinCols), kJoinCols * kJoinParts, 0, s>>>(
+        part, f.rows > 0 ? f.slices : 0, dw, db, (int)f.cols);
     ++g_kernel_launches;
   }
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
@@ -195,15 +597,19 @@ extern "C" sc_status sc_layernorm_forward(const void* X_dev, int dtype, const vo
   if (off(X_dev, elem(dtype)) || off(Y_dev, elem(dtype)) || off(weight_dev, 4) || off(bias_dev, 4) || off(stats_dev, 4) ||
       off(act8_dev, 16))
     return SC_ERR_ALIGNMENT;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return dtype == SC_DTYPE_BF16
-             ? forward<bf16>(X_dev, weight_dev, bias_dev, eps, Y_dev, stats_dev, act8_dev, rows, cols, ldx, ldy, s)
-             : forward<float>(X_dev, weight_dev, bias_dev, eps, Y_dev, stats_dev, act8_dev, rows, cols, ldx, ldy, s);
+  Forward f{};
+  f.X = X_dev; f.Y = Y_dev;
+  f.w = static_cast<const float*>(weight_dev); f.b = static_cast<const float*>(bias_dev);
+  f.eps = eps;
+  f.stats = static_cast<float*>(stats_dev);
+  if (act8_dev) f.a8 = act8_view(act8_dev, rows, cols);
+  f.rows = rows; f.cols = cols; f.ldx = ldx; f.ldy = ldy;
+  return forward(f, dtype, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t sc_layernorm_workspace_bytes(int64_t rows, int64_t cols) {
   if (check_rows(rows, cols) != SC_OK) return 0;
-  return (size_t)norm_slices(rows) * 2 * (size_t)cols * sizeof(float);
+  return (size_t)norm_slices(rows, cols) * 2 * (size_t)cols * sizeof(float);
 }
 
 extern "C" sc_status sc_layernorm_backward(const void* dY_dev, const void* X_dev, int dtype, const void* weight_dev,
@@ -223,10 +629,11 @@ extern "C" sc_status sc_layernorm_backward(const void* dY_dev, const void* X_dev
       off(dbias_dev, 4) || off(workspace, 16))
     return SC_ERR_ALIGNMENT;
   if (rows == 0 && !dweight_dev && !dbias_dev) return SC_OK;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  float* part = static_cast<float*>(workspace);
-  return dtype == SC_DTYPE_BF16 ? backward<bf16>(dY_dev, X_dev, weight_dev, stats_dev, residual_grad_dev, dX_dev,
-                                                 dweight_dev, dbias_dev, rows, cols, lddy, ldx, ldr, lddx, part, s)
-                                : backward<float>(dY_dev, X_dev, weight_dev, stats_dev, residual_grad_dev, dX_dev,
-                                                  dweight_dev, dbias_dev, rows, cols, lddy, ldx, ldr, lddx, part, s);
+  Backward f{};
+  f.dY = dY_dev; f.X = X_dev; f.R = residual_grad_dev; f.dX = dX_dev;
+  f.w = static_cast<const float*>(weight_dev); f.stats = static_cast<const float*>(stats_dev);
+  f.part = static_cast<float*>(workspace);
+  f.rows = rows; f.cols = cols; f.lddy = lddy; f.ldx = ldx; f.ldr = ldr; f.lddx = lddx;
+  return backward(f, dtype, static_cast<float*>(dweight_dev), static_cast<float*>(dbias_dev),
+                  static_cast<cudaStream_t>(stream));
 }
