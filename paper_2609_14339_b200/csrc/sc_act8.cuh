@@ -56,21 +56,35 @@ __device__ __forceinline__ void a8_unpack4(uint32_t w, float step, float* v) {
 }
 
 // ---- activations -----------------------------------------------------------------------------------------------
+// One instruction each (the compiler's own forms spend several on denormal arguments, which cannot matter here: the
+// reciprocal's argument is at least 1, and an exponential that small adds nothing).
+__device__ __forceinline__ float fast_rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
 // Normal distribution function from Hastings' rational approximation of erfc (Abramowitz and Stegun 7.1.26, absolute error
 // 1.5e-7 in erf): for x = |z| / sqrt(2), t = 1 / (1 + p x), erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) exp(-x^2).
-// The lower tail comes out directly, not as 1 - (nearly 1), and the density the slope needs is the same exponential. A
-// third of the instructions of erff, which bounded the kernels that apply it (expand: 92 us with erff for 4096 x 14336).
+// The lower tail comes out directly, not as 1 - (nearly 1), and the density the slope needs is the same exponential. Some
+// 15 instructions, two of them on the special function unit (16 a clock and SM, which bounds the kernels that apply it).
 __device__ __forceinline__ float normal_cdf(float z, float& exp_half_square) {
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-  exp_half_square = __expf(-0.5f * z * z);
-  float p = fmaf(t, 1.061405429f, -1.453152027f);
-  p = fmaf(t, p, 1.421413741f);
-  p = fmaf(t, p, -0.284496736f);
-  p = fmaf(t, p, 0.254829592f);
-  const float tail = 0.5f * t * p * exp_half_square;
+  const float t = fast_rcp(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+  exp_half_square = fast_exp2(z * z * (-0.5f * kLog2e));
+  float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  p = fmaf(t, p, 0.5f * 1.421413741f);
+  p = fmaf(t, p, 0.5f * -0.284496736f);
+  p = fmaf(t, p, 0.5f * 0.254829592f);
+  const float tail = t * p * exp_half_square;
   return z >= 0.f ? 1.f - tail : tail;
 }
+__device__ __forceinline__ float sigmoid(float z) { return fast_rcp(1.f + fast_exp2(z * -kLog2e)); }
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
   if (ACT == SC_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
@@ -78,7 +92,7 @@ __device__ __forceinline__ float act_value(float z) {
     float e;
     return z * normal_cdf(z, e);
   }
-  if (ACT == SC_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+  if (ACT == SC_ACT_SILU) return z * sigmoid(z);
   return z;
 }
 template <int ACT>
@@ -90,7 +104,7 @@ __device__ __forceinline__ float act_slope(float z) {
     return fmaf(z * 0.39894228040143268f, e, c);
   }
   if (ACT == SC_ACT_SILU) {
-    const float s = __fdividef(1.f, 1.f + __expf(-z));
+    const float s = sigmoid(z);
     return s * (1.f + z * (1.f - s));
   }
   return 1.f;

@@ -246,19 +246,6 @@ extern "C" sc_status sc_linear_weight_grad(const void* dY_dev, int operand_dtype
   const int64_t wide = (cols + 31) / 32 * 32;
   const size_t a_bytes = (size_t)tokens * wide * (operand_dtype == SC_DTYPE_FP32 ? 4 : 2);
   float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + (a_bytes + 15) / 16 * 16);
-  if (dbias_dev) {
-    const int slices = tokens < kColSlices ? (int)tokens : kColSlices;
-    const unsigned blocks = (unsigned)((rows + 127) / 128);
-    if (tokens > 0) {
-      if (operand_dtype == SC_DTYPE_FP32)
-        column_sum_kernel<float><<<dim3(blocks, slices), 128, 0, s>>>(static_cast<const float*>(dY_dev), part, tokens, rows, lddy);
-      else
-        column_sum_kernel<bf16><<<dim3(blocks, slices), 128, 0, s>>>(static_cast<const bf16*>(dY_dev), part, tokens, rows, lddy);
-      ++g_kernel_launches;
-    }
-    column_join_kernel<<<blocks, 128, 0, s>>>(part, static_cast<float*>(dbias_dev), slices, rows);
-    ++g_kernel_launches;
-  }
   if (tokens > 0) {
     st = sc_act8_expand(act8_dev, act, workspace, operand_dtype, tokens, cols, wide, stream);
     if (st != SC_OK) return st;
@@ -271,8 +258,26 @@ extern "C" sc_status sc_linear_weight_grad(const void* dY_dev, int operand_dtype
   p.epi.ldo = cols;
   p.epi.out_f32 = out_dtype == SC_DTYPE_FP32;
   p.epi.scale = scale;
-  if (tokens == 0)
+  if (tokens == 0) {
+    if (dbias_dev && cudaMemsetAsync(dbias_dev, 0, (size_t)rows * sizeof(float), s) != cudaSuccess) return SC_ERR_CUDA;
     return cudaMemsetAsync(G_dev, 0, (size_t)rows * (size_t)cols * (out_dtype == SC_DTYPE_FP32 ? 4 : 2), s) == cudaSuccess
                ? SC_OK : SC_ERR_CUDA;
+  }
+  const bool tensor = operand_dtype == SC_DTYPE_BF16 && linear_tc_supported(p);
+  if (dbias_dev && tensor) {            // by the product's own blocks
+    p.epi.dy = dY_dev;
+    p.epi.db = static_cast<float*>(dbias_dev);
+    p.epi.tokens = tokens;
+    p.epi.ld_dy = lddy;
+  } else if (dbias_dev) {
+    const int slices = tokens < kColSlices ? (int)tokens : kColSlices;
+    const unsigned blocks = (unsigned)((rows + 127) / 128);
+    if (operand_dtype == SC_DTYPE_FP32)
+      column_sum_kernel<float><<<dim3(blocks, slices), 128, 0, s>>>(static_cast<const float*>(dY_dev), part, tokens, rows, lddy);
+    else
+      column_sum_kernel<bf16><<<dim3(blocks, slices), 128, 0, s>>>(static_cast<const bf16*>(dY_dev), part, tokens, rows, lddy);
+    column_join_kernel<<<blocks, 128, 0, s>>>(part, static_cast<float*>(dbias_dev), slices, rows);
+    g_kernel_launches += 2;
+  }
   return linear_run(kEpiWeight, operand_dtype == SC_DTYPE_FP32, p, static_cast<unsigned*>(status_dev), s);
 }

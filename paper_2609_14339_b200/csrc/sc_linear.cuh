@@ -22,6 +22,9 @@ struct LinEpilogue {
   int out_f32;
   int act;
   float scale;
+  const void* dy;           // weight, tensor-core engine: db = column sums of dy (tokens x rows of D), or db null
+  float* db;
+  int64_t tokens, ld_dy;
 };
 
 // D[m x n] = sum_k A(m, k) B(n, k); element (i, k) of an operand is at base[i * s_row + k * s_k], one stride is 1.

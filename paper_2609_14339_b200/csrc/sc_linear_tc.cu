@@ -1,16 +1,20 @@
 // Tensor-core engine of the linear layer's three products (see sc_linear.cu for the roles of A and B):
 //   D[m, n] = sum_k A(m, k) B(n, k),  bf16 operands, fp32 accumulation in tensor memory, epilogue fused.
 //
-// linear_pair_kernel    large products: a cluster of two SMs on a 256 x bn tile (tcgen05 cta_group::2), persistent, two
-//                       accumulators in tensor memory so that a tile's epilogue runs under the next tile's MMAs.
-// linear_split_kernel   few rows of D, or few tiles: one SM on a 128 x bn tile of D^T (the contiguous dimension of D on the
-//                       128 accumulator lanes), the contraction split over a cluster of up to 8 blocks that join their
+// linear_pair_kernel    more than 128 rows: two SMs on a 256 x bn tile (tcgen05 cta_group::2). Enough tiles for the chip:
+//                       persistent pairs, two accumulators in tensor memory so that a tile's epilogue runs under the next
+//                       tile's MMAs. Fewer: the contraction is split over the 2 to 4 pairs of a cluster, which join their
 //                       partial sums through distributed shared memory in a fixed order.
+// linear_split_kernel   few rows of D: one SM on a 128 x bn tile of D^T (the contiguous dimension of D on the 128
+//                       accumulator lanes, so that a tile of few rows wastes nothing), the contraction split over a cluster
+//                       of up to 8 blocks, joined the same way.
 //
 // Operands come by TMA in boxes of 64 along k, 128-byte swizzle; an operand whose contraction index is slow in memory is
 // taken as it lies (MN-major descriptor), nothing is transposed. Sizes that end inside a box come in as zeros.
 // Every mbarrier wait is bounded; a wait that runs out latches the time-out bit in *status and the block winds down.
 #include <cuda.h>
+
+#include <mutex>
 
 #include "sc_linear.cuh"
 #include "sc_ptx.cuh"
@@ -43,6 +47,7 @@ struct LtBars {
   uint32_t tmem_slot;
   int abort_flag;
   int never_flag;
+  float red[8][32];              // column sums of dY, one row per epilogue warp
 };
 
 template <int KIND>
@@ -129,19 +134,67 @@ __device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtSha
   }
 }
 
+// ---------------------------------------------------------------------------------------- bias gradient
+// The weight gradient's epilogue warps have nothing to do until the first tile is finished: they sum dY's columns
+// meanwhile, 32 columns per block and turn, the tokens over the threads, joined in a fixed order. dY comes out of L2 for
+// the most part (the pipeline reads it too) and no launch, workspace or second pass is spent on it.
+template <int WARPS>
+__device__ __forceinline__ void bias_gradient(const LinEpilogue& e, int rows, float (*red)[32]) {
+  const int tid = threadIdx.x - 64, warp = tid >> 5, lane = tid & 31, group = tid & 3;
+  const bf16* dy = static_cast<const bf16*>(e.dy);
+  for (int c0 = blockIdx.x * 32; c0 < rows; c0 += gridDim.x * 32) {
+    const int c = c0 + group * 8, n = rows - c;
+    float s[8] = {};
+    for (int64_t t = tid >> 2; t < e.tokens; t += 8 * WARPS * 4) {
+      float x[4][8];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t tt = t + u * 8 * WARPS;
+        load8(dy, 0, tt * e.ld_dy + c, true, tt < e.tokens ? n : 0, x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += x[u][j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 4);
+      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 8);
+      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 16);
+    }
+    if (lane < 4)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) red[warp][lane * 8 + j] = s[j];
+    asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
+    if (warp == 0 && c0 + lane < rows) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) v += red[w][lane];
+      e.db[c0 + lane] = v;
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
+  }
+}
+
 // ---------------------------------------------------------------------------------------- two SMs per 256 x bn tile
-template <int KIND>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLtPairThreads, 1)
+// Launched in clusters of 2 * split blocks; blocks 2p and 2p + 1 are pair p of the cluster.
+template <int KIND, bool SPLIT>
+__global__ void __launch_bounds__(kLtPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                   const __grid_constant__ LtShape sh, const __grid_constant__ LinEpilogue epi, unsigned* status) {
+                   const __grid_constant__ LtShape sh, const __grid_constant__ LinEpilogue epi, int split, unsigned* status) {
   constexpr bool a_mn = Layout<KIND>::a_mn, b_mn = Layout<KIND>::b_mn;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   LtBars* bars = reinterpret_cast<LtBars*>(smem + kLtPairStages * 4 * kLtBox);
   volatile int* abort_flag = &bars->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank();
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const uint32_t cta = cluster_ctarank(), rank = cta & 1, leader = cta & ~1u;      // rank: which half of the pair
+  const int part_k = SPLIT ? (int)(cta >> 1) : 0;                                  // which share of the contraction
+  const int pair = SPLIT ? (int)(blockIdx.x / (2 * split)) : blockIdx.x >> 1;      // first tile of this pair
+  const int n_pairs = SPLIT ? (int)(gridDim.x / (2 * split)) : gridDim.x >> 1;
+  const int k_begin = SPLIT ? (int)((int64_t)sh.kchunks * part_k / split) : 0;
+  const int k_end = SPLIT ? (int)((int64_t)sh.kchunks * (part_k + 1) / split) : sh.kchunks;
   const int tiles = sh.tiles_m * sh.tiles_n, half = sh.bn / 2;
   const int b_boxes = (half + 63) / 64;
   const uint32_t stage_bytes = 2 * kLtBox + (b_mn ? b_boxes * kLtBox : half * 128);     // what TMA writes per block
@@ -165,19 +218,20 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_after();
   const uint32_t tmem_base = bars->tmem_slot;
 
+  const int q = warp & 3, part = (warp - 2) >> 2;      // epilogue warps: quarter of the lanes; every second 32 columns
+  bool dead = false;
   if (warp == 0) {
     if (lane == 0) {
       uint32_t it = 0;
-      bool dead = false;
       for (int tile = pair; tile < tiles && !dead; tile += n_pairs) {
         const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
         const int a_row = tm * 256 + (int)rank * 128, b_row = tn * sh.bn + (int)rank * half;
-        for (int kc = 0; kc < sh.kchunks; ++kc, ++it) {
+        for (int kc = k_begin; kc < k_end; ++kc, ++it) {
           const int s = it % kLtPairStages;
           if (!mbar_wait(&bars->empty[s], ((it / kLtPairStages) & 1) ^ 1, abort_flag)) { dead = true; break; }
           uint8_t* st = smem + (size_t)s * 4 * kLtBox;
           if (rank == 0) mbar_expect_tx(&bars->full[s], 2 * stage_bytes);      // both blocks' bytes
-          const uint32_t leader_bar = map_to_rank(smem_u32(&bars->full[s]), 0);
+          const uint32_t leader_bar = map_to_rank(smem_u32(&bars->full[s]), leader);
           if (a_mn) {
             for (int b = 0; b < 2; ++b) tma_load_2d_pair(st + b * kLtBox, &map_a, leader_bar, a_row + b * 64, kc * kLtK);
           } else {
@@ -210,24 +264,23 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     if (lane == 0 && rank == 0) {
       const uint32_t idesc = umma_idesc_bf16_any(256, sh.bn, a_mn, b_mn);
       uint32_t it = 0, t = 0;
-      bool dead = false;
       for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
         const uint32_t ab = t & 1;
         if (!mbar_wait(&bars->acc_empty[ab], ((t >> 1) & 1) ^ 1, abort_flag)) { dead = true; break; }
         tc_fence_after();
         const uint32_t d = tmem_base + ab * 256;
-        for (int kc = 0; kc < sh.kchunks; ++kc, ++it) {
+        for (int kc = k_begin; kc < k_end; ++kc, ++it) {
           const int s = it % kLtPairStages;
           if (!mbar_wait(&bars->full[s], (it / kLtPairStages) & 1, abort_flag)) { dead = true; break; }
           tc_fence_after();
           const uint32_t a0 = smem_u32(smem + (size_t)s * 4 * kLtBox), b0 = a0 + 2 * kLtBox;
 #pragma unroll
           for (int k = 0; k < kLtK / 16; ++k)
-            umma_bf16_pair(d, lt_desc(a0, a_mn, k), lt_desc(b0, b_mn, k), idesc, (kc | k) != 0);
-          umma_commit_pair(&bars->empty[s]);
+            umma_bf16_pair(d, lt_desc(a0, a_mn, k), lt_desc(b0, b_mn, k), idesc, kc > k_begin || k > 0);
+          umma_commit_pair(&bars->empty[s], leader);
         }
         if (dead) break;
-        umma_commit_pair(&bars->acc_full[ab]);
+        umma_commit_pair(&bars->acc_full[ab], leader);
       }
       if (dead) {
         if (status) atomicOr(status, kDevTimeout);
@@ -240,9 +293,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
     __syncwarp();
   } else {
-    const int q = warp & 3, part = (warp - 2) >> 2;      // lanes of this warp's quarter; every second block of 32 columns
     uint32_t t = 0;
-    bool dead = false;
+    if (KIND == kEpiWeight && epi.db) bias_gradient<8>(epi, sh.M, bars->red);
     for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
       const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
       const uint32_t ab = t & 1;
@@ -250,29 +302,70 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       tc_fence_after();
       const int row = tm * 256 + (int)rank * 128 + q * 32 + lane;
       const uint32_t d = tmem_base + ab * 256 + ((uint32_t)(q * 32) << 16);
-      for (int c = part * 32; c < sh.bn; c += 64) {
-        const int col = tn * sh.bn + c;
-        const bool live = row < sh.M && col < sh.N;
-        float v[32], aux[32];
-        if (live) epilogue_aux32<KIND>(epi, sh, aux, row, col);
-        __syncwarp();
-        tmem_ld32(d + c, v);
-        tmem_ld_wait();
-        if (live) epilogue_row32<KIND>(epi, sh, aux, v, row, col);
-        __syncwarp();
+      if (SPLIT) {         // partial sums to this block's shared memory (the pipeline's, idle by now), column after column
+        float* mine = reinterpret_cast<float*>(smem) + q * 32 + lane;
+        for (int c = part * 32; c < sh.bn; c += 64) {
+          float v[32];
+          tmem_ld32(d + c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) mine[(c + j) * 128] = v[j];
+        }
+      } else {
+        for (int c = part * 32; c < sh.bn; c += 64) {
+          const int col = tn * sh.bn + c;
+          const bool live = row < sh.M && col < sh.N;
+          float v[32], aux[32];
+          if (live) epilogue_aux32<KIND>(epi, sh, aux, row, col);
+          __syncwarp();
+          tmem_ld32(d + c, v);
+          tmem_ld_wait();
+          if (live) epilogue_row32<KIND>(epi, sh, aux, v, row, col);
+          __syncwarp();
+        }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&bars->acc_empty[ab]), 0));   // the leader's barrier
+      if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&bars->acc_empty[ab]), leader));   // the leader's barrier
     }
     if (dead && lane == 0) {
       if (status) atomicOr(status, kDevTimeout);
       *abort_flag = 1;
     }
   }
+  if (SPLIT) {
+    // join: each pair finishes its share of the tile's blocks of 32 columns, adding the pairs' sums in their order
+    __syncwarp();
+    cluster_sync_all();
+    if (warp >= 2) {
+      const int tm = sh.m_fastest ? pair % sh.tiles_m : pair / sh.tiles_n, tn = sh.m_fastest ? pair / sh.tiles_m : pair % sh.tiles_n;
+      const int row = tm * 256 + (int)rank * 128 + q * 32 + lane, blocks = sh.bn / 32;
+      const int last = blocks * (part_k + 1) / split;
+      for (int blk = blocks * part_k / split + part; blk < last; blk += 2) {
+        const int col = tn * sh.bn + blk * 32;
+        if (row < sh.M && col < sh.N) {
+          float v[32], aux[32];
+          epilogue_aux32<KIND>(epi, sh, aux, row, col);
+          const uint32_t at = smem_u32(smem) + (uint32_t)(blk * 32 * 128 + q * 32 + lane) * 4;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0.f;
+          for (int s = 0; s < split; ++s) {
+            const uint32_t from = map_to_rank(at, 2 * s + rank);
+            float w[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w[j] = ld_shared_cluster(from + j * 512);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += w[j];
+          }
+          epilogue_row32<KIND>(epi, sh, aux, v, row, col);
+        }
+      }
+    }
+    __syncwarp();
+  }
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();            // nothing of the peer is touched after this
+  cluster_sync_all();            // nothing of the other blocks is touched after this
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
 }
@@ -428,6 +521,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
     __syncwarp();
   }
 
+  if (KIND == kEpiWeight && epi.db && warp >= 2) bias_gradient<4>(epi, sh.M, bars->red);
   const int q = warp & 3;
   const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16);
   const int col = tn * 128 + q * 32 + lane;
@@ -467,13 +561,17 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
       const int last = first + share < sh.bn ? first + share : sh.bn;
       const uint32_t base = smem_u32(mine) + (q * 32 + lane) * 4;
       for (int c = first; c < last && row0 + c < sh.M; c += 4) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < split; ++s) {
-          const uint32_t from = map_to_rank(base, s);
+        float v[4] = {0.f, 0.f, 0.f, 0.f}, w[8][4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (c + j < last) v[j] += ld_shared_cluster(from + (c + j) * 512);
+        for (int s = 0; s < 8; ++s) {            // all of them on their way before the first is added
+          const uint32_t from = map_to_rank(base, s < split ? s : 0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[s][j] = s < split && c + j < last ? ld_shared_cluster(from + (c + j) * 512) : 0.f;
         }
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] += w[s][j];
         // the rows past this block's share belong to the next block: give them a row outside D
         LtShape mine_sh = sh;
         mine_sh.M = row0 + last < sh.M ? (int)(row0 + last) : sh.M;
@@ -526,37 +624,63 @@ bool encode_operand(CUtensorMap* out, const LinOperand& o, int64_t rows, int64_t
   return o.s_k == 1 ? encode(out, o.base, K, rows, o.s_row, box_rows) : encode(out, o.base, rows, K, o.s_k, kLtK);
 }
 
+constexpr int kMaxDevices = 64;
+constexpr size_t kSplitSmemMax = 227 * 1024;
+size_t pair_smem() { return (size_t)kLtPairStages * 4 * kLtBox + sizeof(LtBars) + 1024; }
+
 struct Device {
   int n_sm = 0;
+  int clusters[5] = {};          // clusters of 2 * split blocks of the pair kernel that fit at once, by split
   bool ready = false;
 };
-constexpr int kMaxDevices = 64;
 
-size_t pair_smem() { return (size_t)kLtPairStages * 4 * kLtBox + sizeof(LtBars) + 1024; }
-constexpr size_t kSplitSmemMax = 227 * 1024;
+cudaLaunchConfig_t config(unsigned blocks, int threads, size_t smem, unsigned cluster, cudaLaunchAttribute* attr, cudaStream_t s) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  attr->id = cudaLaunchAttributeClusterDimension;
+  attr->val.clusterDim.x = cluster;
+  attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cfg;
+}
 
-// SM count of the current device, with the kernels' shared-memory limits raised on it (once per device)
-int device_sms() {
+// What the choice of a kernel needs to know of the current device; raises the kernels' shared-memory limits on the way.
+// Filled once per device.
+const Device* device() {
   static Device devices[kMaxDevices];
+  static std::mutex lock;
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
+  std::lock_guard<std::mutex> hold(lock);
   Device& d = devices[dev];
-  if (!d.ready) {
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    const int pair = (int)pair_smem(), split = (int)kSplitSmemMax;
-    const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    if (cudaFuncSetAttribute(linear_pair_kernel<kEpiForward>, at, pair) != cudaSuccess ||
-        cudaFuncSetAttribute(linear_pair_kernel<kEpiInput>, at, pair) != cudaSuccess ||
-        cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight>, at, pair) != cudaSuccess ||
-        cudaFuncSetAttribute(linear_split_kernel<kEpiForward>, at, split) != cudaSuccess ||
-        cudaFuncSetAttribute(linear_split_kernel<kEpiInput>, at, split) != cudaSuccess ||
-        cudaFuncSetAttribute(linear_split_kernel<kEpiWeight>, at, split) != cudaSuccess)
-      return 0;
-    d.n_sm = n;
-    d.ready = true;            // a second thread that gets here first does the same work to the same end
+  if (d.ready) return &d;
+  Device n;
+  if (cudaDeviceGetAttribute(&n.n_sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n.n_sm < 2) return nullptr;
+  const int pair = (int)pair_smem(), split = (int)kSplitSmemMax;
+  const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  if (cudaFuncSetAttribute(linear_pair_kernel<kEpiForward, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiForward, true>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, true>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, true>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_split_kernel<kEpiForward>, at, split) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_split_kernel<kEpiInput>, at, split) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_split_kernel<kEpiWeight>, at, split) != cudaSuccess)
+    return nullptr;
+  for (int k = 1; k <= 4; ++k) {
+    cudaLaunchAttribute attr{};
+    const cudaLaunchConfig_t cfg = config(2u * k, kLtPairThreads, pair_smem(), 2u * k, &attr, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&n.clusters[k], linear_pair_kernel<kEpiForward, true>, &cfg) != cudaSuccess) return nullptr;
+    if (n.clusters[k] < 1) n.clusters[k] = 1;
   }
-  return d.n_sm;
+  n.ready = true;
+  d = n;
+  return &d;
 }
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -567,43 +691,40 @@ struct Choice {
   double cost = 1e30;
 };
 
-// Clocks of the two kernels for one shape, counted from what bounds a stage: the tensor pipe (2 clocks per column of the
-// tile and stage of 64) or shared memory (each operand byte is written once and read once, 128 bytes a clock).
-Choice choose(int kind, int64_t M, int64_t N, int64_t K, int n_sm) {
+Choice choose(int kind, int64_t M, int64_t N, int64_t K, const Device& d) {
   const int64_t chunks = up(K, kLtK);
   Choice best;
-  for (int bn = 256; bn >= 128; bn -= 32) {
-    const double tiles = (double)up(M, 256) * (double)up(N, bn), waves = (double)(int64_t)((tiles + n_sm / 2 - 1) / (n_sm / 2));
-    const double stage = 2.0 * bn > 2.0 * (128 + bn / 2) ? 2.0 * bn : 2.0 * (128 + bn / 2);
-    const double cost = waves * (double)chunks * stage * 1.1 + 4000.0 + 3000.0;
-    if (cost < best.cost) best = {true, bn, 1, kLtPairStages, cost};
-  }
-  const bool r_mn = kind == kEpiWeight;
-  const int64_t m16 = up(M, 16) * 16;
-  for (int bn = r_mn ? 64 : 16; bn <= 256; bn += r_mn ? 64 : 16) {
-    if (bn > m16 && bn > (r_mn ? 64 : 16) && bn - (r_mn ? 64 : 16) >= m16) break;
-    const size_t stage_bytes = 2 * kLtBox + (size_t)bn * 128;
-    const int per_sm = bn <= 64 ? 2 : 1;
-    int stages = (int)(((per_sm == 2 ? 110 : 220) * 1024) / stage_bytes);
-    if (stages > kLtMaxStages) stages = kLtMaxStages;
-    for (int split = 1; split <= 8; ++split) {
-      if (split > chunks) break;
-      if (split > 1 && (size_t)bn * 512 > (size_t)stages * stage_bytes) break;       // the partial sums' room
-      const double blocks = (double)up(M, bn) * (double)up(N, 128) * split;
-      const double waves = (double)(int64_t)((blocks + n_sm - 1) / n_sm);
-      const double stage = 2.0 * (128 + bn);
-      const double cost = waves * ((double)up(chunks, split) * stage + 1500.0 + 12.0 * bn / split) + (split > 1 ? 1500.0 + 8.0 * bn : 0.0) + 2000.0;
-      if (cost < best.cost) best = {false, bn, split, stages, cost};
+  if (M > 128) {
+    for (int bn = 256; bn >= 128; bn -= 32) {
+      const int64_t tiles = up(M, 256) * up(N, bn);
+      const double stage = 500.0 + bn;
+      for (int split = 1; split <= 4; ++split) {
+        if (split > 1 && (split > chunks || tiles * split > d.n_sm / 2)) break;
+        const double waves = (double)up(tiles, split == 1 ? d.n_sm / 2 : d.clusters[split]);
+        const double cost = waves * ((double)up(chunks, split) * stage + 1500.0) + (split > 1 ? 3000.0 : 0.0);
+        if (cost < best.cost) best = {true, bn, split, kLtPairStages, cost};
+      }
     }
+    return best;
   }
+  const int step = kind == kEpiWeight ? 64 : 16;
+  const int bn = (int)up(M, step) * step;
+  const size_t stage_bytes = 2 * kLtBox + (size_t)bn * 128;
+  const int64_t tiles = up(N, 128);
+  int split = 1;
+  while (split < 8 && tiles * split < d.n_sm && 2 * split <= chunks) split *= 2;
+  int stages = (int)((bn <= 64 ? 110 : 220) * 1024 / stage_bytes);
+  if (stages > kLtMaxStages) stages = kLtMaxStages;
+  while (split > 1 && (size_t)bn * 512 > (size_t)stages * stage_bytes) split /= 2;       // the partial sums' room
+  best = {false, bn, split, stages, 0.0};
   return best;
 }
 
 template <int KIND>
 sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
-  const int n_sm = device_sms();
-  if (n_sm < 2) return SC_ERR_CUDA;
-  const Choice c = choose(KIND, p.M, p.N, p.K, n_sm);
+  const Device* dev = device();
+  if (!dev) return SC_ERR_CUDA;
+  const Choice c = choose(KIND, p.M, p.N, p.K, *dev);
   LtShape sh{};
   sh.M = (int)p.M; sh.N = (int)p.N;
   sh.kchunks = (int)up(p.K, kLtK);
@@ -614,33 +735,27 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
   sh.vec = wide(p.epi.out, p.epi.ldo) && (!p.epi.res || wide(p.epi.res, p.epi.ldr));
   sh.vec_bias = (reinterpret_cast<uintptr_t>(p.epi.bias) & 15) == 0;
   CUtensorMap a, b;
+  cudaLaunchAttribute attr{};
   if (c.pair) {
     sh.tiles_m = (int)up(p.M, 256);
     sh.tiles_n = (int)up(p.N, c.bn);
-    if ((int64_t)sh.tiles_m * sh.tiles_n > 0x7fffffff) return SC_ERR_TOO_LARGE;
+    const int64_t tiles = (int64_t)sh.tiles_m * sh.tiles_n;
+    if (tiles > 0x0fffffff) return SC_ERR_TOO_LARGE;
     sh.m_fastest = p.M <= p.N;
     if (!encode_operand(&a, p.A, p.M, p.K, 128) || !encode_operand(&b, p.B, p.N, p.K, c.bn / 2)) return SC_ERR_CUDA;
-    const int64_t tiles = (int64_t)sh.tiles_m * sh.tiles_n;
-    const int pairs = tiles < n_sm / 2 ? (int)tiles : n_sm / 2;
-    linear_pair_kernel<KIND><<<2 * pairs, kLtPairThreads, pair_smem(), s>>>(a, b, sh, p.epi, status);
+    const int64_t pairs = c.split > 1 ? tiles * c.split : tiles < dev->n_sm / 2 ? tiles : dev->n_sm / 2;
+    const cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, pair_smem(), 2u * c.split, &attr, s);
+    const cudaError_t err = c.split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, sh, p.epi, c.split, status)
+                                        : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, sh, p.epi, 1, status);
+    if (err != cudaSuccess) return SC_ERR_CUDA;
   } else {
     sh.tiles_m = (int)up(p.M, c.bn);
     sh.tiles_n = (int)up(p.N, 128);
     const int64_t blocks = (int64_t)sh.tiles_m * sh.tiles_n * c.split;
     if (blocks > 0x7fffffff) return SC_ERR_TOO_LARGE;
     if (!encode_operand(&a, p.A, p.M, p.K, c.bn) || !encode_operand(&b, p.B, p.N, p.K, 128)) return SC_ERR_CUDA;
-    const size_t r_bytes = KIND == kEpiWeight ? (size_t)up(c.bn, 64) * kLtBox : (size_t)c.bn * 128;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(kLtSplitThreads);
-    cfg.dynamicSmemBytes = (size_t)c.stages * (2 * kLtBox + r_bytes) + sizeof(LtBars) + 1024;
-    cfg.stream = s;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)c.split;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    const size_t smem = (size_t)c.stages * (2 * kLtBox + (size_t)c.bn * 128) + sizeof(LtBars) + 1024;
+    const cudaLaunchConfig_t cfg = config((unsigned)blocks, kLtSplitThreads, smem, (unsigned)c.split, &attr, s);
     if (cudaLaunchKernelEx(&cfg, linear_split_kernel<KIND>, b, a, sh, p.epi, c.split, status) != cudaSuccess) return SC_ERR_CUDA;
   }
   ++g_kernel_launches;

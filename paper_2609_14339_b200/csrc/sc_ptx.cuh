@@ -169,9 +169,9 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t adesc, 
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc), "r"(0u)
       : "memory");
 }
-__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {   // arrives on `bar` in both blocks of the pair
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar, uint32_t leader = 0) {   // arrives on `bar` in both blocks of the pair
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-               ::"r"(smem_u32(bar)), "h"((uint16_t)3)
+               ::"r"(smem_u32(bar)), "h"((uint16_t)(3u << leader))
                : "memory");
 }
 // bf16 x bf16 -> fp32, both operands K-major, M = 256 over the two blocks of a pair.
