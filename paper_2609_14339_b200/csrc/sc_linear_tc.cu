@@ -34,6 +34,7 @@ struct LtShape {
   int kchunks;
   int bn;                  // tile width: columns of D (pair), rows of D (split)
   int tiles_m, tiles_n;    // pair: 256-row x bn-column tiles of D; split: bn-row x 128-column tiles of D
+  int tile_begin, tile_end;    // pair: the tiles of this launch
   int m_fastest;           // pair: which way consecutive tiles run
   int stages;              // split
   int vec;                 // out and res take 16-byte accesses
@@ -136,38 +137,46 @@ __device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtSha
 
 // ---------------------------------------------------------------------------------------- bias gradient
 // The weight gradient's epilogue warps have nothing to do until the first tile is finished: they sum dY's columns
-// meanwhile, 32 columns per block and turn, the tokens over the threads, joined in a fixed order. dY comes out of L2 for
-// the most part (the pipeline reads it too) and no launch, workspace or second pass is spent on it.
-template <int WARPS>
-__device__ __forceinline__ void bias_gradient(const LinEpilogue& e, int rows, float (*red)[32]) {
-  const int tid = threadIdx.x - 64, warp = tid >> 5, lane = tid & 31, group = tid & 3;
+// meanwhile, 8 * G columns per block and turn, the tokens over the threads, joined in a fixed order. dY comes out of L2 for
+// the most part (the pipeline reads it too) and no launch, workspace or second pass is spent on it. G is the widest that
+// still gives every block columns of its own: with 32 columns everywhere, 1024 x 16384 tokens kept 32 of 96 blocks busy
+// for 64 us.
+template <int WARPS, int G>
+__device__ __forceinline__ void bias_gradient_by(const LinEpilogue& e, int rows, float (*red)[32]) {
+  constexpr int LANES = WARPS * 32 / G, UNROLL = 8;            // tokens side by side; tokens per thread and turn
+  const int tid = threadIdx.x - 64, warp = tid >> 5, lane = tid & 31, group = tid % G;
   const bf16* dy = static_cast<const bf16*>(e.dy);
-  for (int c0 = blockIdx.x * 32; c0 < rows; c0 += gridDim.x * 32) {
-    const int c = c0 + group * 8, n = rows - c;
+  for (int64_t c0 = (int64_t)blockIdx.x * 8 * G; c0 < rows; c0 += (int64_t)gridDim.x * 8 * G) {
+    const int64_t c = c0 + group * 8;
     float s[8] = {};
-    for (int64_t t = tid >> 2; t < e.tokens; t += 8 * WARPS * 4) {
-      float x[4][8];
+    if (c + 8 <= rows) {
+      for (int64_t t = tid / G; t < e.tokens; t += LANES * UNROLL) {
+        uint4 x[UNROLL];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t tt = t + u * 8 * WARPS;
-        load8(dy, 0, tt * e.ld_dy + c, true, tt < e.tokens ? n : 0, x[u]);
+        for (int u = 0; u < UNROLL; ++u)
+          x[u] = t + u * LANES < e.tokens ? *reinterpret_cast<const uint4*>(dy + (t + u * LANES) * e.ld_dy + c) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+          const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { s[2 * j] += __uint_as_float(w[j] << 16); s[2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u); }
+        }
       }
+    } else {
+      for (int64_t t = tid / G; t < e.tokens; t += LANES)
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] += x[u][j];
+        for (int j = 0; j < 8; ++j)
+          if (c + j < rows) s[j] += __bfloat162float(dy[t * e.ld_dy + c + j]);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 4);
-      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 8);
-      s[j] += __shfl_xor_sync(0xffffffffu, s[j], 16);
-    }
-    if (lane < 4)
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int o = G; o < 32; o <<= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+    if (lane < G)
 #pragma unroll
       for (int j = 0; j < 8; ++j) red[warp][lane * 8 + j] = s[j];
     asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
-    if (warp == 0 && c0 + lane < rows) {
+    if (warp == 0 && lane < 8 * G && c0 + lane < rows) {
       float v = 0.f;
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) v += red[w][lane];
@@ -175,6 +184,11 @@ __device__ __forceinline__ void bias_gradient(const LinEpilogue& e, int rows, fl
     }
     asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
   }
+}
+template <int WARPS>
+__device__ __forceinline__ void bias_gradient(const LinEpilogue& e, int rows, float (*red)[32]) {
+  if (rows >= 32 * (int)gridDim.x) bias_gradient_by<WARPS, 4>(e, rows, red);
+  else bias_gradient_by<WARPS, 1>(e, rows, red);
 }
 
 // ---------------------------------------------------------------------------------------- two SMs per 256 x bn tile
@@ -191,11 +205,11 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t cta = cluster_ctarank(), rank = cta & 1, leader = cta & ~1u;      // rank: which half of the pair
   const int part_k = SPLIT ? (int)(cta >> 1) : 0;                                  // which share of the contraction
-  const int pair = SPLIT ? (int)(blockIdx.x / (2 * split)) : blockIdx.x >> 1;      // first tile of this pair
+  const int pair = sh.tile_begin + (SPLIT ? (int)(blockIdx.x / (2 * split)) : (int)(blockIdx.x >> 1));   // this pair's first tile
   const int n_pairs = SPLIT ? (int)(gridDim.x / (2 * split)) : gridDim.x >> 1;
   const int k_begin = SPLIT ? (int)((int64_t)sh.kchunks * part_k / split) : 0;
   const int k_end = SPLIT ? (int)((int64_t)sh.kchunks * (part_k + 1) / split) : sh.kchunks;
-  const int tiles = sh.tiles_m * sh.tiles_n, half = sh.bn / 2;
+  const int tiles = sh.tile_end, half = sh.bn / 2;
   const int b_boxes = (half + 63) / 64;
   const uint32_t stage_bytes = 2 * kLtBox + (b_mn ? b_boxes * kLtBox : half * 128);     // what TMA writes per block
 
@@ -217,6 +231,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   cluster_sync_all();            // the peer's barriers exist before anything is sent to them
   tc_fence_after();
   const uint32_t tmem_base = bars->tmem_slot;
+  // the launch of the remaining tiles, if there is one, may take the SMs that this one leaves (see launch())
+  if (!SPLIT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   const int q = warp & 3, part = (warp - 2) >> 2;      // epilogue warps: quarter of the lanes; every second 32 columns
   bool dead = false;
@@ -366,6 +382,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();            // nothing of the other blocks is touched after this
+  // a launch of remaining tiles runs beside the one before it, but must not be over before that one is
+  if (SPLIT) asm volatile("griddepcontrol.wait;" ::: "memory");
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
 }
@@ -735,7 +753,7 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
   sh.vec = wide(p.epi.out, p.epi.ldo) && (!p.epi.res || wide(p.epi.res, p.epi.ldr));
   sh.vec_bias = (reinterpret_cast<uintptr_t>(p.epi.bias) & 15) == 0;
   CUtensorMap a, b;
-  cudaLaunchAttribute attr{};
+  cudaLaunchAttribute attr[2] = {};
   if (c.pair) {
     sh.tiles_m = (int)up(p.M, 256);
     sh.tiles_n = (int)up(p.N, c.bn);
@@ -743,11 +761,35 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
     if (tiles > 0x0fffffff) return SC_ERR_TOO_LARGE;
     sh.m_fastest = p.M <= p.N;
     if (!encode_operand(&a, p.A, p.M, p.K, 128) || !encode_operand(&b, p.B, p.N, p.K, c.bn / 2)) return SC_ERR_CUDA;
-    const int64_t pairs = c.split > 1 ? tiles * c.split : tiles < dev->n_sm / 2 ? tiles : dev->n_sm / 2;
-    const cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, pair_smem(), 2u * c.split, &attr, s);
-    const cudaError_t err = c.split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, sh, p.epi, c.split, status)
-                                        : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, sh, p.epi, 1, status);
-    if (err != cudaSuccess) return SC_ERR_CUDA;
+    const int slots = dev->n_sm / 2;
+    const auto go = [&](int64_t begin, int64_t end, int split, bool rest) {
+      sh.tile_begin = (int)begin;
+      sh.tile_end = (int)end;
+      const int64_t pairs = split > 1 ? (end - begin) * split : end - begin < slots ? end - begin : slots;
+      LinEpilogue epi = p.epi;
+      if (rest) epi.db = nullptr;
+      cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, pair_smem(), 2u * split, attr, s);
+      if (rest) {
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.numAttrs = 2;
+      }
+      ++g_kernel_launches;
+      return split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, sh, epi, split, status)
+                       : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, sh, epi, 1, status);
+    };
+    // The last wave of a launch that needs more than one is seldom full. Where every one of its tiles can have two to four
+    // pairs, it becomes a launch of its own with the contraction split, which starts on the SMs the full waves leave
+    // (4096 x 4096 x 14336, 256 tiles on 74 pairs: 3.5 waves instead of 4).
+    const int64_t full = tiles / slots * slots, rest = tiles - full;
+    int rest_split = 1;
+    if (c.split == 1 && full > 0 && rest > 0)
+      for (int k = 2; k <= 4 && rest <= dev->clusters[k] && sh.kchunks >= 16 * k; ++k) rest_split = k;
+    if (rest_split > 1) {
+      if (go(0, full, 1, false) != cudaSuccess || go(full, tiles, rest_split, true) != cudaSuccess) return SC_ERR_CUDA;
+    } else if (go(0, tiles, c.split, false) != cudaSuccess) {
+      return SC_ERR_CUDA;
+    }
   } else {
     sh.tiles_m = (int)up(p.M, c.bn);
     sh.tiles_n = (int)up(p.N, 128);
@@ -755,10 +797,10 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
     if (blocks > 0x7fffffff) return SC_ERR_TOO_LARGE;
     if (!encode_operand(&a, p.A, p.M, p.K, c.bn) || !encode_operand(&b, p.B, p.N, p.K, 128)) return SC_ERR_CUDA;
     const size_t smem = (size_t)c.stages * (2 * kLtBox + (size_t)c.bn * 128) + sizeof(LtBars) + 1024;
-    const cudaLaunchConfig_t cfg = config((unsigned)blocks, kLtSplitThreads, smem, (unsigned)c.split, &attr, s);
+    const cudaLaunchConfig_t cfg = config((unsigned)blocks, kLtSplitThreads, smem, (unsigned)c.split, attr, s);
     if (cudaLaunchKernelEx(&cfg, linear_split_kernel<KIND>, b, a, sh, p.epi, c.split, status) != cudaSuccess) return SC_ERR_CUDA;
+    ++g_kernel_launches;
   }
-  ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }
 
