@@ -5,106 +5,249 @@
 //   input     A = dY (k fast)              B = W (n fast)              M = tokens, N = cols, K = rows
 //   weight    A = dY (m fast)              B = act(v) (n fast)         M = rows,   N = cols, K = tokens
 #include "sc_linear.cuh"
+#include "sc_ptx.cuh"
 
 namespace sc {
 namespace {
 
-constexpr int kSimtTile = 64, kSimtK = 16;
+constexpr int kSimtM = 64, kSimtN = 128, kSimtK = 16;
 
-template <typename T>
-__device__ __forceinline__ float lin_ld(const void* p, int64_t i) { return (float)static_cast<const T*>(p)[i]; }
-
-__device__ __forceinline__ float epi_read(const void* p, int f32, int64_t i) {
-  return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const bf16*>(p)[i]);
-}
-__device__ __forceinline__ void epi_write(void* p, int f32, int64_t i, float v) {
-  if (f32) static_cast<float*>(p)[i] = v;
-  else static_cast<bf16*>(p)[i] = __float2bfloat16_rn(v);
-}
-
-// CUDA-core product in fp32: 64 x 64 tiles, 4 x 4 sums per thread, any strides. Serves fp32 operands and layouts that
-// TMA cannot describe.
-template <int KIND, typename T, bool A_KFAST, bool B_KFAST>
-__global__ void __launch_bounds__(256)
-linear_simt_kernel(const LinProblem p) {
-  __shared__ float As[kSimtK][kSimtTile + 4], Bs[kSimtK][kSimtTile + 4];
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int64_t tiles_n = (p.N + kSimtTile - 1) / kSimtTile;
-  const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * kSimtTile, n0 = (int64_t)(blockIdx.x % tiles_n) * kSimtTile;
-  float acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < p.K; k0 += kSimtK) {
+// four neighbouring elements, n of them inside the row; vec: 8- or 16-byte accesses where all four are
+__device__ __forceinline__ void load4(const void* p, int f32, int64_t i, bool vec, int n, float* r) {
+  if (f32) {
+    const float* s = static_cast<const float*>(p) + i;
+    if (vec && n == 4) {
+      const float4 f = *reinterpret_cast<const float4*>(s);
+      r[0] = f.x; r[1] = f.y; r[2] = f.z; r[3] = f.w;
+    } else {
 #pragma unroll
-    for (int i = tid; i < kSimtTile * kSimtK; i += 256) {
-      const int ra = A_KFAST ? i / kSimtK : i % kSimtTile, ka = A_KFAST ? i % kSimtK : i / kSimtTile;
-      const int rb = B_KFAST ? i / kSimtK : i % kSimtTile, kb = B_KFAST ? i % kSimtK : i / kSimtTile;
-      As[ka][ra] = (m0 + ra < p.M && k0 + ka < p.K) ? lin_ld<T>(p.A.base, (m0 + ra) * p.A.s_row + (k0 + ka) * p.A.s_k) : 0.f;
-      Bs[kb][rb] = (n0 + rb < p.N && k0 + kb < p.K) ? lin_ld<T>(p.B.base, (n0 + rb) * p.B.s_row + (k0 + kb) * p.B.s_k) : 0.f;
+      for (int j = 0; j < 4; ++j) r[j] = j < n ? s[j] : 0.f;
     }
-    __syncthreads();
+  } else {
+    const bf16* s = static_cast<const bf16*>(p) + i;
 #pragma unroll
-    for (int k = 0; k < kSimtK; ++k) {
-      const float4 a = *reinterpret_cast<const float4*>(&As[k][ty * 4]), b = *reinterpret_cast<const float4*>(&Bs[k][tx * 4]);
-      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
-    }
-    __syncthreads();
+    for (int j = 0; j < 4; ++j) r[j] = j < n ? __bfloat162float(s[j]) : 0.f;
   }
+}
+__device__ __forceinline__ void store4(void* p, int f32, int64_t i, bool vec, int n, const float* v) {
+  if (f32) {
+    float* o = static_cast<float*>(p) + i;
+    if (vec && n == 4) {
+      *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < n) o[j] = v[j];
+    }
+  } else {
+    bf16* o = static_cast<bf16*>(p) + i;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) o[j] = __float2bfloat16_rn(v[j]);
+  }
+}
+
+// CUDA-core product in fp32: 64 x 128 tiles, 8 x 8 sums per thread, any strides. Serves fp32 operands and layouts that
+// TMA cannot describe. Bound by instruction issue: with 8 x 8 sums four of five instructions are multiply-adds, with 4 x 4
+// half of them (300 x 1001 x 999: 40 us then). Few tiles (that result has 40) would leave SMs idle and each block a long
+// serial sum, so the contraction is split over a cluster of up to 8 blocks, joined through distributed shared memory in a
+// fixed order; the next 16 terms are in flight (registers) while the present ones are summed.
+constexpr int kSimtThreads = 128;
+struct SimtTile {
+  float a[kSimtK][kSimtM + 4], b[kSimtK][kSimtN + 4];
+};
+
+// This thread's elements of a ROWS x 16 operand tile. K fast: a warp takes 4 rows x 8 terms at a time (whole sectors, and
+// no two lanes in one bank of the transposed store); otherwise 32 rows of one term. Element j lies a constant number of
+// rows and terms from element 0, so an address is one multiply-add.
+template <typename T, bool KFAST, int ROWS>
+struct SimtLoader {
+  static constexpr int kEach = ROWS * kSimtK / kSimtThreads, kBlocks = ROWS / 32;
+  const T* at;                   // element 0 of the tile to come
+  int64_t s_slow;                // stride of the dimension that is not contiguous
+  int row, term;                 // element 0's place in the tile
+  int rows_left;                 // rows of the operand from the tile's first on
+  int64_t K;
+  float x[kEach];
+  __device__ SimtLoader(const LinOperand& o, int64_t rows, int64_t K_, int64_t row0, int64_t k0) : K(K_) {
+    const int u = (threadIdx.x >> 5) * kEach, lane = threadIdx.x & 31;
+    row = KFAST ? (u >> 1) * 4 + (lane >> 3) : (u % kBlocks) * 32 + lane;
+    term = KFAST ? (lane & 7) : u / kBlocks;
+    s_slow = KFAST ? o.s_row : o.s_k;
+    const int64_t left = rows - row0;
+    rows_left = left < ROWS ? (int)left : ROWS;
+    at = static_cast<const T*>(o.base) + (row0 + row) * o.s_row + (k0 + term) * o.s_k;
+  }
+  __device__ static constexpr int drow(int j) { return KFAST ? (j >> 1) * 4 : (j % kBlocks) * 32; }
+  __device__ static constexpr int dterm(int j) { return KFAST ? (j & 1) * 8 : j / kBlocks; }
+  // the tile from term k0 on; moves on to the next
+  __device__ void load(int64_t k0) {
+    const int k_left = K - k0 < kSimtK ? (int)(K - k0) : kSimtK;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const T* src = KFAST ? at + drow(j) * s_slow + dterm(j) : at + dterm(j) * s_slow + drow(j);
+      x[j] = row + drow(j) < rows_left && term + dterm(j) < k_left ? (float)*src : 0.f;
+    }
+    at += KFAST ? kSimtK : kSimtK * s_slow;
+  }
+  __device__ void store(float (*s)[ROWS + 4]) const {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) s[term + dterm(j)][row + drow(j)] = x[j];
+  }
+};
+
+// what becomes of 4 neighbouring sums of row m, columns n..n+3; all 32 lanes of a warp call it together
+template <int KIND>
+__device__ __forceinline__ void simt_epilogue(const LinProblem& p, float* v, int64_t m, int64_t n, int tx, bool vec) {
   const LinEpilogue& e = p.epi;
-  const int64_t n = n0 + tx * 4;
+  const int64_t room = p.N - n;
+  const int left = m < p.M && room > 0 ? (room < 4 ? (int)room : 4) : 0;
+  float aux[4] = {0.f, 0.f, 0.f, 0.f};
+  if (KIND == kEpiForward && e.res) load4(e.res, e.out_f32, m * e.ldr + n, vec, left, aux);
+  if (KIND == kEpiInput && e.q && left > 0) {
+    a8_unpack4(*reinterpret_cast<const uint32_t*>(e.q + m * e.wide + n), a8_step(e.e[m * (e.wide / 32) + n / 32]), aux);
+    act_slopes<4>(e.act, aux);
+  }
+  if (KIND == kEpiForward) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t m = m0 + ty * 4 + i;
-    float v[4];
+    for (int j = 0; j < 4; ++j) v[j] = j < room ? v[j] + (e.bias ? __ldg(e.bias + n + j) : 0.f) : 0.f;
+    if (e.q) {              // 8 neighbouring threads hold a block of 32 columns
+      uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = acc[i][j];
-    if (KIND == kEpiForward) {
+      for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (e.bias && n + j < p.N) v[j] += e.bias[n + j];
-        if (n + j >= p.N) v[j] = 0.f;
-      }
-      if (e.q) {              // 8 neighbouring threads hold a block of 32 columns
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-#pragma unroll
-        for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const uint32_t eb = a8_scale_byte(top);
-        if (m < p.M && n < e.wide) {
-          *reinterpret_cast<uint32_t*>(e.q + m * e.wide + n) = a8_pack4(v[0], v[1], v[2], v[3], a8_inverse(eb));
-          if ((tx & 7) == 0) e.e[m * (e.wide / 32) + n / 32] = (uint8_t)eb;
-        }
+      for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const uint32_t eb = a8_scale_byte(top);
+      if (m < p.M && n < e.wide) {
+        *reinterpret_cast<uint32_t*>(e.q + m * e.wide + n) = a8_pack4(v[0], v[1], v[2], v[3], a8_inverse(eb));
+        if ((tx & 7) == 0) e.e[m * (e.wide / 32) + n / 32] = (uint8_t)eb;
       }
     }
-    if (m >= p.M) continue;
-    float s[4];
-    if (KIND == kEpiInput && e.q && n < e.wide)
-      a8_unpack4(*reinterpret_cast<const uint32_t*>(e.q + m * e.wide + n), a8_step(e.e[m * (e.wide / 32) + n / 32]), s);
+    act_values<4>(e.act, v);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (n + j >= p.N) break;
-      float y = v[j];
-      if (KIND == kEpiForward) {
-        y = act_value_rt(e.act, y);
-        if (e.res) y += epi_read(e.res, e.out_f32, m * e.ldr + n + j);
-      } else if (KIND == kEpiInput) {
-        if (e.q) y *= act_slope_rt(e.act, s[j]);
-      } else {
-        y *= e.scale;
+    for (int j = 0; j < 4; ++j) v[j] += aux[j];
+  } else if (KIND == kEpiInput) {
+    if (e.q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] *= aux[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= e.scale;
+  }
+  store4(e.out, e.out_f32, m * e.ldo + n, vec, left, v);
+}
+
+template <int KIND, typename T, bool A_KFAST, bool B_KFAST>
+__global__ void __launch_bounds__(kSimtThreads)
+linear_simt_kernel(const __grid_constant__ LinProblem p, unsigned split) {
+  __shared__ __align__(16) union {
+    SimtTile tile[2];
+    float4 sums[kSimtM][kSimtN / 4];
+  } sm;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;         // rows ty * 4 and 32 + ty * 4, columns tx * 4 and 64 + tx * 4
+  const unsigned part = blockIdx.x % split;
+  const unsigned t = blockIdx.x / split, tiles_n = (unsigned)((p.N + kSimtN - 1) / kSimtN);
+  const int64_t m0 = (int64_t)(t / tiles_n) * kSimtM, n0 = (int64_t)(t % tiles_n) * kSimtN;
+  const unsigned steps = (unsigned)((p.K + kSimtK - 1) / kSimtK);           // at most 2^26
+  const int64_t first = steps * part / split, last = steps * (part + 1) / split;
+  SimtLoader<T, A_KFAST, kSimtM> la(p.A, p.M, p.K, m0, first * kSimtK);
+  SimtLoader<T, B_KFAST, kSimtN> lb(p.B, p.N, p.K, n0, first * kSimtK);
+  float acc[8][8] = {};
+  if (first < last) {
+    la.load(first * kSimtK);
+    lb.load(first * kSimtK);
+  }
+  int buf = 0;
+  for (int64_t step = first; step < last; ++step, buf ^= 1) {
+    la.store(sm.tile[buf].a);
+    lb.store(sm.tile[buf].b);
+    __syncthreads();           // the other buffer's readers passed the barrier of the step before
+    if (step + 1 < last) {
+      la.load((step + 1) * kSimtK);
+      lb.load((step + 1) * kSimtK);
+    }
+#pragma unroll 8
+    for (int k = 0; k < kSimtK; ++k) {
+      float av[8], bv[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 a = *reinterpret_cast<const float4*>(&sm.tile[buf].a[k][h * 32 + ty * 4]);
+        const float4 b = *reinterpret_cast<const float4*>(&sm.tile[buf].b[k][h * 64 + tx * 4]);
+        av[4 * h] = a.x; av[4 * h + 1] = a.y; av[4 * h + 2] = a.z; av[4 * h + 3] = a.w;
+        bv[4 * h] = b.x; bv[4 * h + 1] = b.y; bv[4 * h + 2] = b.z; bv[4 * h + 3] = b.w;
       }
-      epi_write(e.out, e.out_f32, m * e.ldo + n + j, y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
     }
   }
+  // The tile's partial sums go to shared memory; each block of the cluster adds up its share of the rows. A lone block
+  // takes the same way: the epilogue then exists once, in a loop (unrolled over the registers it was 15 us of instruction
+  // fetches for the smallest call).
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      sm.sums[(i >> 2) * 32 + ty * 4 + (i & 3)][h * 16 + tx] =
+          make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
+  if (split > 1) cluster_sync_all();
+  else __syncthreads();
+  const int begin = (int)(kSimtM * part / split), end = (int)(kSimtM * (part + 1) / split);
+  const bool vec = p.epi.ldo % 4 == 0 && p.epi.ldr % 4 == 0 &&
+                   ((reinterpret_cast<uintptr_t>(p.epi.out) | reinterpret_cast<uintptr_t>(p.epi.res)) & 15) == 0;
+#pragma unroll 2
+  for (int i0 = begin * 2; i0 < end * 2; i0 += kSimtThreads / 16) {                 // half a row per 16 threads; whole warps
+    const int i = i0 + ty, r = i >> 1, c = (i & 1) * 16 + tx;
+    const bool mine = i < end * 2;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (mine && split > 1) {
+      const uint32_t at = smem_u32(&sm.sums[r][c]);
+      float4 w[8];
+#pragma unroll
+      for (unsigned s = 0; s < 8; ++s)              // all of them on their way before the first is added
+        if (s < split) w[s] = ld_shared_cluster4(map_to_rank(at, s));
+#pragma unroll
+      for (unsigned s = 0; s < 8; ++s)
+        if (s < split) { v[0] += w[s].x; v[1] += w[s].y; v[2] += w[s].z; v[3] += w[s].w; }
+    } else if (mine) {
+      const float4 f = sm.sums[r][c];
+      v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+    }
+    simt_epilogue<KIND>(p, v, mine ? m0 + r : p.M, n0 + c * 4, tx, vec);
+  }
+  if (split > 1) cluster_sync_all();            // the peers have read this block's sums
 }
 
 template <int KIND, typename T>
 sc_status simt_kind(const LinProblem& p, cudaStream_t s) {
-  const int64_t tiles = ((p.M + kSimtTile - 1) / kSimtTile) * ((p.N + kSimtTile - 1) / kSimtTile);
-  if (tiles > 0x7fffffff) return SC_ERR_TOO_LARGE;
-  linear_simt_kernel<KIND, T, KIND != kEpiWeight, KIND == kEpiForward><<<(unsigned)tiles, 256, 0, s>>>(p);
+  const int64_t tiles = ((p.M + kSimtM - 1) / kSimtM) * ((p.N + kSimtN - 1) / kSimtN);
+  const int64_t steps = (p.K + kSimtK - 1) / kSimtK;
+  // Clocks of the SM with the most blocks, from measured ones: a step of one block alone takes 2500 (its four warps wait for
+  // shared memory and for each other), of two side by side 2800, of three 3200; the epilogue 600 for each of a block's
+  // share of 16 turns, a join 2500.
+  int split = 1;
+  double best = 1e30;
+  for (int k = 1; k <= 8 && k <= steps; k += k == 6 ? 2 : 1) {        // clusters of 7 fit the chip badly
+    const int64_t per_sm = (tiles * k + 147) / 148, rounds = (per_sm + 2) / 3, beside = per_sm < 3 ? per_sm : 3;
+    const double step = beside == 1 ? 2500.0 : beside == 2 ? 2800.0 : 3200.0;
+    const double cost = (double)rounds * ((double)((steps + k - 1) / k) * step + 600.0 * (16 / k + 1) + (k > 1 ? 2500.0 : 0.0));
+    if (cost < best) { best = cost; split = k; }
+  }
+  if (tiles * split > 0x7fffffff) return SC_ERR_TOO_LARGE;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(tiles * split));
+  cfg.blockDim = dim3(kSimtThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)split;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, linear_simt_kernel<KIND, T, KIND != kEpiWeight, KIND == kEpiForward>, p, (unsigned)split) != cudaSuccess)
+    return SC_ERR_CUDA;
   ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }

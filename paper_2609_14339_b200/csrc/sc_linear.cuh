@@ -45,21 +45,4 @@ sc_status linear_tc(int kind, const LinProblem& p, unsigned* status, cudaStream_
 
 sc_status linear_simt(int kind, int operand_f32, const LinProblem& p, cudaStream_t s);
 
-__device__ __forceinline__ float act_value_rt(int act, float z) {
-  switch (act) {
-    case SC_ACT_RELU: return act_value<SC_ACT_RELU>(z);
-    case SC_ACT_GELU: return act_value<SC_ACT_GELU>(z);
-    case SC_ACT_SILU: return act_value<SC_ACT_SILU>(z);
-    default: return z;
-  }
-}
-__device__ __forceinline__ float act_slope_rt(int act, float z) {
-  switch (act) {
-    case SC_ACT_RELU: return act_slope<SC_ACT_RELU>(z);
-    case SC_ACT_GELU: return act_slope<SC_ACT_GELU>(z);
-    case SC_ACT_SILU: return act_slope<SC_ACT_SILU>(z);
-    default: return 1.f;
-  }
-}
-
 }  // namespace sc

@@ -18,7 +18,6 @@ from .binding import (SC_ACT_GELU, SC_ACT_NONE, SC_ACT_RELU, SC_ACT_SILU, SC_DTY
 ACTIVATIONS = {"none": SC_ACT_NONE, "relu": SC_ACT_RELU, "gelu": SC_ACT_GELU, "silu": SC_ACT_SILU}
 _DTYPES = {torch.bfloat16: SC_DTYPE_BF16, torch.float32: SC_DTYPE_FP32}
 _F32, _U8 = torch.float32, torch.uint8
-_empty = torch.empty
 
 
 class _Elsewhere:
@@ -141,7 +140,14 @@ class Act8:
 
     @classmethod
     def empty(cls, tokens: int, features: int, device="cuda:0") -> "Act8":
-        return cls(tokens, features, _empty((cls.nbytes(tokens, features),), dtype=_U8, device=device))
+        return cls(tokens, features, torch.empty((cls.nbytes(tokens, features),), dtype=_U8, device=device))
+
+    @classmethod
+    def _new(cls, tokens, features, data):
+        """Of a buffer that has just been made for it."""
+        self = object.__new__(cls)
+        self.tokens, self.features, self.data = tokens, features, data
+        return self
 
     @staticmethod
     def nbytes(tokens: int, features: int) -> int:
@@ -169,11 +175,11 @@ def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, save=None, out=None
     a8 = None if save is None else _saved("save", save, rows, cols, dev)
     with _on(dev, stream):
         if out is None:
-            out, ldy = _empty((rows, cols), dtype=dt, device=X.device), cols
+            out, ldy = X.new_empty((rows, cols)), cols
         else:
             ldy = _matrix("out", out, rows, cols, dt, dev)[2]
         if stats is None:
-            stats = _empty((2, rows), dtype=_F32, device=X.device)
+            stats = X.new_empty((2, rows), dtype=_F32)
         _done(load_library().sc_layernorm_forward(X.data_ptr(), _DTYPES[dt], w, b, eps, out.data_ptr(),
                                                   _stats(stats, rows, dev), a8, rows, cols, ldx, ldy, _raw_stream(dev)),
               "sc_layernorm_forward")
@@ -196,15 +202,15 @@ def layer_norm_backward(dY, X, weight, stats, residual_grad=None, out=None, dwei
     need = lib.sc_layernorm_workspace_bytes(rows, cols)
     with _on(dev, stream):
         if out is None:
-            out, lddx = _empty((rows, cols), dtype=dt, device=X.device), cols
+            out, lddx = X.new_empty((rows, cols)), cols
         else:
             lddx = _matrix("out", out, rows, cols, dt, dev)[2]
         if dweight is None:
-            dweight = _empty((cols,), dtype=_F32, device=X.device)
+            dweight = stats.new_empty((cols,))
         if dbias is None:
-            dbias = _empty((cols,), dtype=_F32, device=X.device)
+            dbias = stats.new_empty((cols,))
         if workspace is None:
-            workspace = _empty((need,), dtype=_U8, device=X.device)
+            workspace = X.new_empty((need,), dtype=_U8)
         _done(lib.sc_layernorm_backward(dY.data_ptr(), X.data_ptr(), _DTYPES[dt], w, st, r, out.data_ptr(),
                                         _vector("dweight", dweight, cols, dev), _vector("dbias", dbias, cols, dev), rows,
                                         cols, lddy, ldx, ldr, lddx, _buffer("workspace", workspace, need, dev),
@@ -218,7 +224,7 @@ def act8_compress(X, out=None, stream=None) -> Act8:
     dev = X.get_device()
     with _on(dev, stream):
         if out is None:
-            out = Act8.empty(tokens, features, X.device)
+            out = Act8._new(tokens, features, X.new_empty((Act8.nbytes(tokens, features),), dtype=_U8))
         _done(load_library().sc_act8_compress(X.data_ptr(), _DTYPES[X.dtype], _saved("out", out, tokens, features, dev),
                                               tokens, features, ldx, _raw_stream(dev)), "sc_act8_compress")
     return out
@@ -233,7 +239,7 @@ def act8_expand(saved, act="none", out=None, out_dtype=torch.bfloat16, stream=No
     dev = data.get_device()
     with _on(dev, stream):
         if out is None:
-            out = _empty((tokens, features), dtype=_out_dtype(None, out_dtype, None), device=data.device)
+            out = data.new_empty((tokens, features), dtype=_out_dtype(None, out_dtype, None))
         ldy = _matrix("out", out, tokens, features, None, dev)[2]
         _done(load_library().sc_act8_expand(data.data_ptr(), a, out.data_ptr(), _DTYPES[out.dtype], tokens, features, ldy,
                                             _raw_stream(dev)), "sc_act8_expand")
@@ -248,7 +254,7 @@ def act8_backward(dA, saved, act, out=None, stream=None):
     a8 = _saved("saved", saved, tokens, features, dev)
     with _on(dev, stream):
         if out is None:
-            out = _empty((tokens, features), dtype=dt, device=dA.device)
+            out = dA.new_empty((tokens, features))
         lddz = _matrix("out", out, tokens, features, dt, dev)[2]
         _done(load_library().sc_act8_backward(dA.data_ptr(), a8, a, out.data_ptr(), _DTYPES[dt], tokens, features, ldda,
                                               lddz, _raw_stream(dev)), "sc_act8_backward")
@@ -272,7 +278,7 @@ def linear(X, W, bias=None, residual=None, act="none", save=None, out=None, out_
     a8 = None if save is None else _saved("save", save, tokens, rows, dev)
     with _on(dev, stream):
         if out is None:
-            out, ldy = _empty((tokens, rows), dtype=odt, device=X.device), rows
+            out, ldy = X.new_empty((tokens, rows), dtype=odt), rows
         else:
             ldy = _matrix("out", out, tokens, rows, None, dev)[2]
         _done(load_library().sc_linear_forward(X.data_ptr(), W.data_ptr(), _DTYPES[dt], b, r, out.data_ptr(), _DTYPES[odt],
@@ -292,7 +298,7 @@ def linear_backward_input(dY, W, saved=None, act="none", out=None, out_dtype=Non
     a8 = None if saved is None else _saved("saved", saved, tokens, cols, dev)
     with _on(dev, stream):
         if out is None:
-            out, lddx = _empty((tokens, cols), dtype=odt, device=dY.device), cols
+            out, lddx = dY.new_empty((tokens, cols), dtype=odt), cols
         else:
             lddx = _matrix("out", out, tokens, cols, None, dev)[2]
         _done(load_library().sc_linear_backward_input(dY.data_ptr(), W.data_ptr(), _DTYPES[dt], a8, a, out.data_ptr(),
@@ -320,13 +326,13 @@ def linear_weight_grad(dY, saved, act="none", scale: float = 1.0, out=None, out_
         raise SCError(-2, "sc_linear_weight_grad_workspace_bytes")
     with _on(dev, stream):
         if out is None:
-            out = _empty((rows, cols), dtype=odt, device=dY.device)
+            out = dY.new_empty((rows, cols), dtype=odt)
         elif _matrix("out", out, rows, cols, None, dev)[2] != cols:
             raise ValueError("out must be contiguous")
         if dbias is None:
-            dbias = _empty((rows,), dtype=_F32, device=dY.device)
+            dbias = dY.new_empty((rows,), dtype=_F32)
         if workspace is None:
-            workspace = _empty((need,), dtype=_U8, device=dY.device)
+            workspace = dY.new_empty((need,), dtype=_U8)
         _done(lib.sc_linear_weight_grad(dY.data_ptr(), _DTYPES[dt], a8, a, scale, out.data_ptr(), _DTYPES[odt],
                                         _vector("dbias", dbias, rows, dev), tokens, rows, cols, lddy,
                                         _buffer("workspace", workspace, need, dev), workspace.numel(),
