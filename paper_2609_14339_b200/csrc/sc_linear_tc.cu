@@ -728,10 +728,14 @@ Choice choose(int kind, int64_t M, int64_t N, int64_t K, const Device& d) {
   const int step = kind == kEpiWeight ? 64 : 16;
   const int bn = (int)up(M, step) * step;
   const size_t stage_bytes = 2 * kLtBox + (size_t)bn * 128;
+  // Enough blocks for every SM, two or three of them side by side: one's loads cover another's join. A tile of more than 64
+  // rows that can have three quarters of the SMs without a split is better off without (128 x 14336 x 4096: 36 us, split
+  // in two 41 us); fewer than 33 rows leave room for three blocks per SM (1 x 14336 x 4096: 24.2 us, two blocks 25.2).
   const int64_t tiles = up(N, 128);
   int split = 1;
-  while (split < 8 && tiles * split < d.n_sm && 2 * split <= chunks) split *= 2;
-  int stages = (int)((bn <= 64 ? 110 : 220) * 1024 / stage_bytes);
+  if (bn <= 64 || 4 * tiles < 3 * d.n_sm)
+    while (split < 8 && tiles * split < d.n_sm && 2 * split <= chunks) split *= 2;
+  int stages = (int)((bn <= 32 ? 74 : bn > 64 && split == 1 ? 220 : 110) * 1024 / stage_bytes);
   if (stages > kLtMaxStages) stages = kLtMaxStages;
   while (split > 1 && (size_t)bn * 512 > (size_t)stages * stage_bytes) split /= 2;       // the partial sums' room
   best = {false, bn, split, stages, 0.0};

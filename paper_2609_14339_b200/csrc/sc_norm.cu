@@ -56,6 +56,41 @@ __device__ __forceinline__ void block_sums(float& a, float& b, float (*red)[2][3
   b = __shfl_sync(0xffffffffu, v, 16);
 }
 
+// Two fp32 operations in one instruction: these kernels are bound by issue slots before HBM.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 f2_make(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ f2 f2_make(float a) { return f2_make(a, a); }
+__device__ __forceinline__ float2 f2_get(f2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f2 f2_add(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 f2_mul(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 f2_fma(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
 // A thread's EPT columns of one row, as they lie in memory. VEC: EPT neighbours from thread * EPT on in 16-byte accesses
 // (the number of columns is a multiple of EPT, so a thread's columns are all inside the row or all outside); otherwise
 // every blockDim-th column, one at a time (any stride, alignment and width, still coalesced). Outside the row: zeros.
@@ -79,6 +114,7 @@ struct Piece {
       for (int i = 0; i < EPT; ++i) w[i] = in(i, cols) ? __float_as_uint(ld1<F32>(p, at + col(i))) : 0u;
     }
   }
+  __device__ f2 pair(int i) const { return f2_make(get(2 * i), get(2 * i + 1)); }
   __device__ float get(int i) const {
     if (!VEC || F32) return __uint_as_float(w[i]);
     return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
@@ -143,16 +179,29 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
                     float* __restrict__ stats, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int64_t wide, int64_t rows,
                     int cols, int64_t ldx, int64_t ldy) {
   extern __shared__ float4 param_smem[];
-  __shared__ float red[2][2][32];
+  __shared__ float2 red[2][2][32];
   typedef Piece<F32, EPT, VEC> P;
   typedef Params<EPT, THREADS> W;
-  constexpr int ROWS = EPT == 16 ? 1 : 2;
+  constexpr int ROWS = EPT == 16 ? 1 : 2, WARPS = THREADS / 32;
   W* pw = reinterpret_cast<W*>(param_smem);
   W* pb = pw + 1;
   pw->template fill<VEC>(weight, cols, 1.f);
   pb->template fill<VEC>(bias, cols, 0.f);
   int turn = 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float n = (float)cols, inv_n = 1.f / n;
+  // columns of this thread's warp, and of the warp this lane stands for in the join
+  const auto columns_of = [&](int w) {
+    if (!VEC) {          // EPT runs of 32 columns, THREADS apart
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) c += min(32, max(0, cols - i * THREADS - w * 32));
+      return (float)c;
+    }
+    return (float)min(32 * EPT, max(0, cols - w * 32 * EPT));
+  };
+  const float n_warp = columns_of(warp), inv_n_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
+  const float n_lane = lane < WARPS ? columns_of(lane) : 0.f;
   P ahead[ROWS];
   const int64_t groups = (rows + ROWS - 1) / ROWS;
   const auto fetch = [&](int64_t g) {
@@ -166,41 +215,64 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
   };
   fetch(blockIdx.x);
   for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
-    P x[ROWS];
-#pragma unroll
-    for (int h = 0; h < ROWS; ++h) x[h] = ahead[h];
-    fetch(g + gridDim.x);
-    float s[2] = {0.f, 0.f}, mean[2], rstd[2];
+    f2 x[ROWS][EPT / 2];
 #pragma unroll
     for (int h = 0; h < ROWS; ++h)
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) s[h] += x[h].get(i);
-    block_sums(s[0], s[1], red, turn);
+      for (int i = 0; i < EPT / 2; ++i) x[h][i] = ahead[h].pair(i);
+    fetch(g + gridDim.x);
+    // Mean and squared deviations of each warp's columns, then joined exactly: sum_w M2_w + n_w (mean_w - mean)^2. As
+    // accurate as a second pass with the row's mean, with one barrier instead of two.
+    float mean[ROWS], m2[ROWS];
 #pragma unroll
     for (int h = 0; h < ROWS; ++h) {
-      mean[h] = mean_of(s[h], n, inv_n);
-      s[h] = 0.f;
+      f2 s = x[h][0];
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        const float d = VEC || P::in(i, cols) ? x[h].get(i) - mean[h] : 0.f;
-        s[h] = fmaf(d, d, s[h]);
+      for (int i = 1; i < EPT / 2; ++i) s = f2_add(s, x[h][i]);
+      const float2 p = f2_get(s);
+      mean[h] = mean_of(warp_sum(p.x + p.y), n_warp, inv_n_warp);
+      const f2 minus = f2_make(-mean[h]);
+      f2 v = f2_make(0.f);
+#pragma unroll
+      for (int i = 0; i < EPT / 2; ++i) {
+        f2 d = f2_add(x[h][i], minus);
+        if (!VEC) {
+          const float2 e = f2_get(d);
+          d = f2_make(P::in(2 * i, cols) ? e.x : 0.f, P::in(2 * i + 1, cols) ? e.y : 0.f);
+        }
+        v = f2_fma(d, d, v);
       }
-      if (VEC && !P::in(0, cols)) s[h] = 0.f;
+      const float2 e = f2_get(v);
+      m2[h] = warp_sum(VEC && !P::in(0, cols) ? 0.f : e.x + e.y);
     }
-    block_sums(s[0], s[1], red, turn);
+    if (WARPS > 1) {
+      if (lane == 0)
+#pragma unroll
+        for (int h = 0; h < ROWS; ++h) red[turn][h][warp] = make_float2(mean[h], m2[h]);
+      __syncthreads();           // the other half of red is free: its readers passed this barrier a turn ago
+#pragma unroll
+      for (int h = 0; h < ROWS; ++h) {
+        const float2 w = lane < WARPS ? red[turn][h][lane] : make_float2(0.f, 0.f);
+        mean[h] = mean_of(warp_sum(n_lane * w.x), n, inv_n);
+        const float d = w.x - mean[h];
+        m2[h] = warp_sum(n_lane > 0.f ? fmaf(n_lane * d, d, w.y) : 0.f);
+      }
+      turn ^= 1;
+    }
 #pragma unroll
     for (int h = 0; h < ROWS; ++h) {
       const int64_t r = ROWS * g + h;
-      rstd[h] = rsqrtf(s[h] * inv_n + eps);
+      const float rstd = rsqrtf(fmaf(m2[h], inv_n, eps));
       if (ROWS > 1 && r >= rows) continue;
-      if (stats && threadIdx.x == 0) { stats[r] = mean[h]; stats[rows + r] = rstd[h]; }
+      if (stats && threadIdx.x == 0) { stats[r] = mean[h]; stats[rows + r] = rstd; }
+      const f2 minus = f2_make(-mean[h]), scale = f2_make(rstd);
       float y[EPT];            // outside the row: 0 (weight and bias are 0 there)
 #pragma unroll
       for (int k = 0; k < EPT / 4; ++k) {
         const float4 w = pw->get(k), b = pb->get(k);
-        const float wv[4] = {w.x, w.y, w.z, w.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[4 * k + i] = fmaf((x[h].get(4 * k + i) - mean[h]) * rstd[h], wv[i], bv[i]);
+        const float2 lo = f2_get(f2_fma(f2_add(x[h][2 * k], minus), f2_mul(scale, f2_make(w.x, w.y)), f2_make(b.x, b.y)));
+        const float2 hi = f2_get(f2_fma(f2_add(x[h][2 * k + 1], minus), f2_mul(scale, f2_make(w.z, w.w)), f2_make(b.z, b.w)));
+        y[4 * k] = lo.x; y[4 * k + 1] = lo.y; y[4 * k + 2] = hi.x; y[4 * k + 3] = hi.y;
       }
       if (q) {                 // blocks of 32 columns: 32 / EPT neighbouring threads, or the 32 lanes of a warp
         if (VEC) {
@@ -250,9 +322,9 @@ norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ we
   int turn = 0;
   const float inv_n = 1.f / (float)cols;
   pw.template fill<VEC>(weight, cols, 1.f);
-  float sw[EPT], sb[EPT];
+  f2 sw[EPT / 2], sb[EPT / 2];
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) sw[i] = sb[i] = 0.f;
+  for (int i = 0; i < EPT / 2; ++i) sw[i] = sb[i] = f2_make(0.f);
   P nx, ny, nr;
   float n_mean = 0.f, n_rstd = 0.f;
   const auto fetch = [&](int64_t r) {
@@ -270,33 +342,37 @@ norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ we
     P res = nr;
     if (!RES_AHEAD && R) res.load(R, r * ldr, cols);
     if (AHEAD && r + gridDim.x < rows) fetch(r + gridDim.x);
-    float s0 = 0.f, s1 = 0.f;
+    const f2 minus = f2_make(-mean), scale = f2_make(rstd);
+    f2 s0 = f2_make(0.f), s1 = f2_make(0.f);
 #pragma unroll
     for (int k = 0; k < EPT / 4; ++k) {
       const float4 w4 = pw.get(k);
-      const float w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 4 * k + j;
-        const float d = dy.get(i), n = (x.get(i) - mean) * rstd, g = d * w[j];        // outside the row d = 0
-        s0 += g;
-        s1 = fmaf(g, n, s1);
-        sw[i] = fmaf(d, n, sw[i]);
-        sb[i] += d;
+      for (int h = 0; h < 2; ++h) {
+        const int i = 2 * k + h;
+        const f2 w = h ? f2_make(w4.z, w4.w) : f2_make(w4.x, w4.y);
+        const f2 d = dy.pair(i), nn = f2_mul(f2_add(x.pair(i), minus), scale), g = f2_mul(d, w);      // outside the row d = 0
+        s0 = f2_add(s0, g);
+        s1 = f2_fma(g, nn, s1);
+        sw[i] = f2_fma(d, nn, sw[i]);
+        sb[i] = f2_add(sb[i], d);
       }
     }
-    block_sums(s0, s1, red, turn);
-    const float m0 = s0 * inv_n, m1 = s1 * inv_n;
+    const float2 p0 = f2_get(s0), p1 = f2_get(s1);
+    float t0 = p0.x + p0.y, t1 = p1.x + p1.y;
+    block_sums(t0, t1, red, turn);
+    const f2 minus_m0 = f2_make(-t0 * inv_n), minus_m1 = f2_make(-t1 * inv_n);
     float v[EPT];
 #pragma unroll
     for (int k = 0; k < EPT / 4; ++k) {
       const float4 w4 = pw.get(k);
-      const float w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 4 * k + j;
-        const float n = (x.get(i) - mean) * rstd, t = fmaf(-n, m1, fmaf(dy.get(i), w[j], -m0));
-        v[i] = fmaf(t, rstd, R ? res.get(i) : 0.f);
+      for (int h = 0; h < 2; ++h) {
+        const int i = 2 * k + h;
+        const f2 w = h ? f2_make(w4.z, w4.w) : f2_make(w4.x, w4.y);
+        const f2 nn = f2_mul(f2_add(x.pair(i), minus), scale), t = f2_fma(nn, minus_m1, f2_fma(dy.pair(i), w, minus_m0));
+        const float2 o = f2_get(f2_fma(t, scale, R ? res.pair(i) : f2_make(0.f)));
+        v[2 * i] = o.x; v[2 * i + 1] = o.y;
       }
     }
     store_piece<F32, EPT, VEC>(dX, r * lddx, cols, v);
@@ -305,8 +381,9 @@ norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ we
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
       if (P::in(i, cols)) {
-        part[((size_t)blockIdx.x * 2 + 0) * cols + P::col(i)] = sw[i];
-        part[((size_t)blockIdx.x * 2 + 1) * cols + P::col(i)] = sb[i];
+        const float2 a = f2_get(sw[i / 2]), b = f2_get(sb[i / 2]);
+        part[((size_t)blockIdx.x * 2 + 0) * cols + P::col(i)] = i & 1 ? a.y : a.x;
+        part[((size_t)blockIdx.x * 2 + 1) * cols + P::col(i)] = i & 1 ? b.y : b.x;
       }
     }
   }
