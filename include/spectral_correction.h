@@ -314,8 +314,9 @@ SC_API sc_status sc_layernorm_backward(const void* dY_dev, const void* X_dev, in
  * clamped to +-127 and stands for that integer times 2^e, which bf16 represents exactly: a checkpoint that has been
  * expanded to bf16 loses nothing. The error is at most 2^e / 2 (2^e for a value that was clamped), at most 1/64 of the
  * block's largest value. A block that holds an infinity or a NaN stands for NaNs.
- * Layout of a checkpoint (16-byte aligned): tokens x F int8, F = features rounded up to 32 (the padding is zero),
- * then, from the next multiple of 256 bytes, tokens x F/32 bytes e + 127 (255: a block of NaNs). */
+ * Layout of a checkpoint (16-byte aligned): for each block of 32 features in turn (the last one padded with zeros), 32
+ * int8 per token; then, from the next multiple of 256 bytes, for each block one byte e + 127 per token (255: a block of
+ * NaNs). */
 SC_API size_t sc_act8_bytes(int64_t tokens, int64_t features);
 SC_API sc_status sc_act8_compress(const void* X_dev, int dtype, void* act8_dev, int64_t tokens, int64_t features,
                                   int64_t ldx, void* stream);

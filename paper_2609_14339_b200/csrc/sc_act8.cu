@@ -7,46 +7,35 @@ namespace {
 
 constexpr int kA8Unroll = 4;
 
-// Work is cut into units of 8 features (four neighbouring lanes hold a block of 32). A thread takes kA8Unroll units at a
-// time, all of them loaded before the first is used: HBM latency times bandwidth is some 45 KB per SM, and one unit per
-// thread in flight leaves much of it idle.
-// FLAT: no row ends inside a unit's block and rows follow one another without a gap in the tensor and the checkpoint, so
-// the unit's number is all that is needed; otherwise row and column advance from unit to unit without a division.
-template <bool FLAT>
-struct A8Walk {
-  int64_t row, unit, step;
-  int col8, step_col8, units_row;
-  int64_t step_row;
-  __device__ A8Walk(int64_t wide) {
-    unit = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    step = (int64_t)gridDim.x * blockDim.x;
-    if (!FLAT) {
-      units_row = (int)(wide / 8);
-      row = unit / units_row;
-      col8 = (int)(unit - row * units_row);
-      step_row = step / units_row;
-      step_col8 = (int)(step - step_row * units_row);
-    }
+// A warp takes 32 tokens of one block of 32 features, 8 tokens at a time with four lanes a token and 8 features a lane; a
+// thread block's 8 warps take neighbouring blocks of features. All addresses follow from three pointers by constant
+// strides: with a walk that computed them anew (some 50 instructions for 8 values) instruction issue was the bound, 48 us
+// for 4096 x 14336 instead of 30. The four loads of a lane are all on their way before the first is used: HBM latency
+// times bandwidth is some 45 KB per SM.
+struct A8Place {
+  int64_t token;             // of the first of kA8Unroll turns, 8 tokens apart
+  int col, left;             // left: tokens from there to the end
+  int64_t at, scale_at;      // in the checkpoint
+  bool live;
+  __device__ A8Place(int64_t tokens, int blocks) {
+    const unsigned across = (unsigned)(blocks + 7) / 8, ty = blockIdx.x / across, tx = blockIdx.x - ty * across;
+    const int block = (int)tx * 8 + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    token = (int64_t)ty * (8 * kA8Unroll) + (lane >> 2);
+    left = tokens - token < 8 * kA8Unroll ? (int)(tokens - token) : 8 * kA8Unroll;
+    col = block * 32 + (lane & 3) * 8;
+    live = block < blocks;               // the same for the whole warp
+    scale_at = (int64_t)block * tokens + token;
+    at = scale_at * 32 + (lane & 3) * 8;
   }
-  __device__ void next() {
-    unit += step;
-    if (!FLAT) {
-      row += step_row;
-      col8 += step_col8;
-      if (col8 >= units_row) { col8 -= units_row; ++row; }
-    }
-  }
-  __device__ int64_t at(int64_t ld) const { return FLAT ? unit * 8 : row * ld + col8 * 8; }
-  __device__ int left(int features) const { return FLAT ? 8 : features - col8 * 8; }
 };
 // 8 elements as they lie in memory (16 or 32 bytes), loaded before they are converted
 template <bool F32>
 struct Raw8 {
   uint4 w[F32 ? 2 : 1];
-  __device__ void load(const void* p, int64_t i) {
+  __device__ void load(const void* p, int64_t i, bool live) {
     const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * (F32 ? 4 : 2));
-    w[0] = src[0];
-    if (F32) w[1] = src[1];
+    w[0] = live ? src[0] : make_uint4(0u, 0u, 0u, 0u);
+    if (F32) w[1] = live ? src[1] : make_uint4(0u, 0u, 0u, 0u);
   }
   __device__ void get(float* x) const {
     const uint32_t* r = reinterpret_cast<const uint32_t*>(w);
@@ -55,111 +44,105 @@ struct Raw8 {
       x[j] = F32 ? __uint_as_float(r[j]) : __uint_as_float(j & 1 ? r[j / 2] & 0xffff0000u : r[j / 2] << 16);
   }
 };
-
-__device__ __forceinline__ void a8_write_unit(const float* x, int8_t* q, uint8_t* qe, int64_t unit, bool live) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  const uint32_t e = a8_scale_byte(top);
-  const float inv = a8_inverse(e);
-  if (live) {
-    reinterpret_cast<uint2*>(q)[unit] = make_uint2(a8_pack4(x[0], x[1], x[2], x[3], inv), a8_pack4(x[4], x[5], x[6], x[7], inv));
-    if ((threadIdx.x & 3) == 0) qe[unit / 4] = (uint8_t)e;
+// VEC: every row's 8 elements are 16-byte aligned and all inside the row or all outside (features a multiple of 8);
+// otherwise they are converted as they come.
+template <bool F32, bool VEC>
+struct Eight {
+  Raw8<F32> raw;
+  float x[VEC ? 1 : 8];
+  __device__ void load(const void* p, int64_t i, int n) {
+    if (VEC) raw.load(p, i, n > 0);
+    else load8(p, F32, i, false, n, x);
   }
-}
-
-// units: tokens * wide / 8. A checkpoint's rows follow one another without a gap, so a unit's number is its place in it.
-template <bool F32, bool FLAT>
-__global__ void __launch_bounds__(256)
-a8_compress_kernel(const void* __restrict__ X, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int64_t wide,
-                   int64_t units, int features, int64_t ldx, bool vec) {
-  A8Walk<FLAT> w(wide);
-  // whole warps leave together: the shuffles need them (units is a multiple of 4, not of 32)
-  while (__any_sync(0xffffffffu, w.unit < units)) {
-    const int64_t unit0 = w.unit;
-    if (FLAT) {
-      Raw8<F32> r[kA8Unroll];
-#pragma unroll
-      for (int u = 0; u < kA8Unroll; ++u) {
-        if (w.unit < units) r[u].load(X, w.unit * 8);
-        else r[u] = Raw8<F32>{};
-        w.next();
-      }
-#pragma unroll
-      for (int u = 0; u < kA8Unroll; ++u) {
-        float x[8];
-        r[u].get(x);
-        a8_write_unit(x, q, qe, unit0 + u * w.step, unit0 + u * w.step < units);
-      }
+  __device__ void get(float* v) const {
+    if (VEC) {
+      raw.get(v);
     } else {
-      float x[kA8Unroll][8];
 #pragma unroll
-      for (int u = 0; u < kA8Unroll; ++u) {
-        load8(X, F32, w.at(ldx), vec, w.unit < units ? w.left(features) : 0, x[u]);
-        w.next();
-      }
+      for (int j = 0; j < 8; ++j) v[j] = x[VEC ? 0 : j];
+    }
+  }
+};
+
+template <bool F32, bool VEC>
+__global__ void __launch_bounds__(256)
+a8_compress_kernel(const void* __restrict__ X, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int blocks,
+                   int64_t tokens, int features, int64_t ldx) {
+  const A8Place p(tokens, blocks);
+  if (!p.live) return;
+  const int64_t at = p.token * ldx + p.col;
+  Eight<F32, VEC> x[kA8Unroll];
 #pragma unroll
-      for (int u = 0; u < kA8Unroll; ++u) a8_write_unit(x[u], q, qe, unit0 + u * w.step, unit0 + u * w.step < units);
+  for (int u = 0; u < kA8Unroll; ++u) x[u].load(X, at + u * 8 * ldx, u * 8 < p.left ? features - p.col : 0);
+#pragma unroll
+  for (int u = 0; u < kA8Unroll; ++u) {
+    float v[8];
+    x[u].get(v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t e = a8_scale_byte(top);
+    const float inv = a8_inverse(e);
+    if (u * 8 < p.left) {
+      *reinterpret_cast<uint2*>(q + p.at + u * 256) =
+          make_uint2(a8_pack4(v[0], v[1], v[2], v[3], inv), a8_pack4(v[4], v[5], v[6], v[7], inv));
+      if ((threadIdx.x & 3) == 0) qe[p.scale_at + u * 8] = (uint8_t)e;
     }
   }
 }
 
 // Y = act(v), or GRAD: Y = dA * act'(v). dA and Y may be the same matrix.
-template <bool F32, int ACT, bool GRAD, bool FLAT>
+template <bool F32, int ACT, bool GRAD, bool VEC>
 __global__ void __launch_bounds__(256)
-a8_expand_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ qe, int64_t wide, const void* dA, void* Y,
-                 int64_t units, int features, int64_t ldda, int64_t ldy, bool vec) {
-  A8Walk<FLAT> w(wide);
-  while (w.unit < units) {
-    A8Walk<FLAT> o = w;
-    uint2 b[kA8Unroll];
-    uint32_t e[kA8Unroll];
-    Raw8<F32> raw[GRAD && FLAT ? kA8Unroll : 1];
+a8_expand_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ qe, int blocks, const void* dA, void* Y,
+                 int64_t tokens, int features, int64_t ldda, int64_t ldy) {
+  const A8Place p(tokens, blocks);
+  if (!p.live || p.col >= features) return;
+  const int64_t from = p.token * ldda + p.col, to = p.token * ldy + p.col;
+  const int n = features - p.col;
+  uint2 b[kA8Unroll];
+  uint32_t e[kA8Unroll];
+  Eight<F32, VEC> d[GRAD ? kA8Unroll : 1];
 #pragma unroll
-    for (int u = 0; u < kA8Unroll; ++u) {
-      if (w.unit < units) {
-        b[u] = __ldcs(reinterpret_cast<const uint2*>(q) + w.unit);
-        e[u] = qe[w.unit / 4];
-        if (GRAD && FLAT) raw[u].load(dA, w.unit * 8);
-      }
-      w.next();
+  for (int u = 0; u < kA8Unroll; ++u) {
+    b[u] = make_uint2(0u, 0u);
+    e[u] = 0;
+    if (u * 8 < p.left) {
+      b[u] = __ldcs(reinterpret_cast<const uint2*>(q + p.at + u * 256));
+      e[u] = qe[p.scale_at + u * 8];
+      if (GRAD) d[u].load(dA, from + u * 8 * ldda, n);
     }
+  }
 #pragma unroll
-    for (int u = 0; u < kA8Unroll; ++u) {
-      const int n = o.unit < units ? o.left(features) : 0;
-      if (n > 0) {
-        float v[8], a[8];
-        if (GRAD && FLAT) raw[u].get(a);
-        if (GRAD && !FLAT) load8(dA, F32, o.at(ldda), vec, n, a);
-        a8_unpack4(b[u].x, a8_step(e[u]), v);
-        a8_unpack4(b[u].y, a8_step(e[u]), v + 4);
+  for (int u = 0; u < kA8Unroll; ++u) {
+    if (u * 8 < p.left) {
+      float v[8], a[8];
+      if (GRAD) d[u].get(a);
+      a8_unpack4(b[u].x, a8_step(e[u]), v);
+      a8_unpack4(b[u].y, a8_step(e[u]), v + 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = GRAD ? a[j] * act_slope<ACT>(v[j]) : act_value<ACT>(v[j]);
-        store8(Y, F32, o.at(ldy), vec, n, v);
-      }
-      o.next();
+      for (int j = 0; j < 8; ++j) v[j] = GRAD ? a[j] * act_slope<ACT>(v[j]) : act_value<ACT>(v[j]);
+      store8(Y, F32, to + u * 8 * ldy, VEC, n, v);
     }
   }
 }
 
-unsigned grid_for(int64_t units) {
-  const int64_t g = (units + 256 * kA8Unroll - 1) / (256 * kA8Unroll), most = 148 * 16;
-  return (unsigned)(g < most ? g : most);
+// 0: more blocks than a grid has
+unsigned grid_for(int64_t tokens, int64_t wide) {
+  const int64_t g = ((tokens + 8 * kA8Unroll - 1) / (8 * kA8Unroll)) * ((wide / 32 + 7) / 8);
+  return g <= 0x7fffffff ? (unsigned)g : 0u;
 }
-bool vec_ok(const void* p, int64_t ld, int dtype) {
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * (dtype == SC_DTYPE_BF16 ? 2 : 4)) % 16 == 0;
-}
-// one stretch of memory whose blocks of 32 are the checkpoint's (a single row of full blocks too)
-bool flat_ok(const void* p, int64_t ld, int64_t tokens, int64_t features) {
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && features % 32 == 0 && (ld == features || tokens == 1);
+bool vec_ok(const void* p, int64_t ld, int64_t features, int dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * (dtype == SC_DTYPE_BF16 ? 2 : 4)) % 16 == 0 && features % 8 == 0;
 }
 
 sc_status check(const void* act8, int dtype, int64_t tokens, int64_t features) {
   if (dtype != SC_DTYPE_BF16 && dtype != SC_DTYPE_FP32) return SC_ERR_DTYPE;
   if (tokens < 0 || features <= 0) return SC_ERR_SHAPE;
-  if (tokens > (1 << 30) || features > (1 << 30)) return SC_ERR_TOO_LARGE;
+  if (tokens > (1 << 30) || features > (1 << 30) || (tokens > 0 && grid_for(tokens, (features + 31) / 32 * 32) == 0))
+    return SC_ERR_TOO_LARGE;
   if (tokens > 0 && !act8) return SC_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(act8) & 15) return SC_ERR_ALIGNMENT;
   return SC_OK;
@@ -169,15 +152,12 @@ bool off(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (d
 template <bool F32, int ACT, bool GRAD>
 void expand_one(const Act8View& v, const void* dA, void* Y, int64_t tokens, int64_t features, int64_t ldda, int64_t ldy,
                 cudaStream_t s) {
-  const int dtype = F32 ? SC_DTYPE_FP32 : SC_DTYPE_BF16;
-  const int64_t units = tokens * (v.wide / 8);
-  const unsigned grid = grid_for(units);
-  if (flat_ok(Y, ldy, tokens, features) && (!GRAD || flat_ok(dA, ldda, tokens, features))) {
-    a8_expand_kernel<F32, ACT, GRAD, true><<<grid, 256, 0, s>>>(v.q, v.e, v.wide, dA, Y, units, (int)features, ldda, ldy, true);
-  } else {
-    const bool vec = vec_ok(Y, ldy, dtype) && (!GRAD || vec_ok(dA, ldda, dtype));
-    a8_expand_kernel<F32, ACT, GRAD, false><<<grid, 256, 0, s>>>(v.q, v.e, v.wide, dA, Y, units, (int)features, ldda, ldy, vec);
-  }
+  const int dtype = F32 ? SC_DTYPE_FP32 : SC_DTYPE_BF16, blocks = (int)(v.wide / 32);
+  const unsigned grid = grid_for(tokens, v.wide);
+  if (vec_ok(Y, ldy, features, dtype) && (!GRAD || vec_ok(dA, ldda, features, dtype)))
+    a8_expand_kernel<F32, ACT, GRAD, true><<<grid, 256, 0, s>>>(v.q, v.e, blocks, dA, Y, tokens, (int)features, ldda, ldy);
+  else
+    a8_expand_kernel<F32, ACT, GRAD, false><<<grid, 256, 0, s>>>(v.q, v.e, blocks, dA, Y, tokens, (int)features, ldda, ldy);
 }
 template <bool F32, bool GRAD>
 void expand_act(const Act8View& v, int act, const void* dA, void* Y, int64_t tokens, int64_t features, int64_t ldda,
@@ -211,17 +191,16 @@ extern "C" sc_status sc_act8_compress(const void* X_dev, int dtype, void* act8_d
   if (!X_dev) return SC_ERR_INVALID_ARG;
   if (off(X_dev, dtype)) return SC_ERR_ALIGNMENT;
   const Act8View v = act8_view(act8_dev, tokens, features);
-  const int64_t units = tokens * (v.wide / 8);
-  const unsigned grid = grid_for(units);
-  const bool vec = vec_ok(X_dev, ldx, dtype), flat = flat_ok(X_dev, ldx, tokens, features);
-  const int n = (int)features;
+  const unsigned grid = grid_for(tokens, v.wide);
+  const bool vec = vec_ok(X_dev, ldx, features, dtype);
+  const int n = (int)features, blocks = (int)(v.wide / 32);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == SC_DTYPE_BF16) {
-    if (flat) a8_compress_kernel<false, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
-    else a8_compress_kernel<false, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
+    if (vec) a8_compress_kernel<false, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
+    else a8_compress_kernel<false, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
   } else {
-    if (flat) a8_compress_kernel<true, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
-    else a8_compress_kernel<true, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, v.wide, units, n, ldx, vec);
+    if (vec) a8_compress_kernel<true, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
+    else a8_compress_kernel<true, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
   }
   ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;

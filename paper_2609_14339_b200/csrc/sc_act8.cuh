@@ -8,18 +8,25 @@ namespace sc {
 
 constexpr int kA8Block = 32;
 
-struct Act8View {           // a checkpoint's two parts
-  int8_t* q;                // tokens x wide
-  uint8_t* e;               // tokens x wide / 32
-  int64_t wide;             // features rounded up to 32
+// A checkpoint's two parts. Blocks of features are the slow index: block b of all tokens, 32 bytes a token, then block
+// b + 1; the scale bytes lie the same way. A warp that holds 32 tokens' values of one block (a GEMM epilogue) then reads
+// or writes 1 KB in one piece, and one that holds one token's (rows are 32 lanes there) 32 bytes, a whole sector.
+struct Act8View {
+  int8_t* q;
+  uint8_t* e;
+  int64_t tokens, wide;     // wide: features rounded up to 32
 };
 inline Act8View act8_view(void* blob, int64_t tokens, int64_t features) {
   Act8View v;
+  v.tokens = tokens;
   v.wide = (features + kA8Block - 1) / kA8Block * kA8Block;
   v.q = static_cast<int8_t*>(blob);
   v.e = static_cast<uint8_t*>(blob) + (tokens * v.wide + 255) / 256 * 256;
   return v;
 }
+// places of feature f of token t, and of its block's scale byte
+__device__ __forceinline__ int64_t a8_at(int64_t tokens, int64_t t, int64_t f) { return ((f >> 5) * tokens + t) * 32 + (f & 31); }
+__device__ __forceinline__ int64_t a8_scale_at(int64_t tokens, int64_t t, int64_t f) { return (f >> 5) * tokens + t; }
 
 // Scale byte of a block from the largest |x| (as bits; NaN and infinity compare above every finite value).
 __device__ __forceinline__ uint32_t a8_scale_byte(uint32_t amax_bits) {

@@ -105,7 +105,7 @@ __device__ __forceinline__ void simt_epilogue(const LinProblem& p, float* v, int
   float aux[4] = {0.f, 0.f, 0.f, 0.f};
   if (KIND == kEpiForward && e.res) load4(e.res, e.out_f32, m * e.ldr + n, vec, left, aux);
   if (KIND == kEpiInput && e.q && left > 0) {
-    a8_unpack4(*reinterpret_cast<const uint32_t*>(e.q + m * e.wide + n), a8_step(e.e[m * (e.wide / 32) + n / 32]), aux);
+    a8_unpack4(*reinterpret_cast<const uint32_t*>(e.q + a8_at(p.M, m, n)), a8_step(e.e[a8_scale_at(p.M, m, n)]), aux);
     act_slopes<4>(e.act, aux);
   }
   if (KIND == kEpiForward) {
@@ -119,8 +119,8 @@ __device__ __forceinline__ void simt_epilogue(const LinProblem& p, float* v, int
       for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
       const uint32_t eb = a8_scale_byte(top);
       if (m < p.M && n < e.wide) {
-        *reinterpret_cast<uint32_t*>(e.q + m * e.wide + n) = a8_pack4(v[0], v[1], v[2], v[3], a8_inverse(eb));
-        if ((tx & 7) == 0) e.e[m * (e.wide / 32) + n / 32] = (uint8_t)eb;
+        *reinterpret_cast<uint32_t*>(e.q + a8_at(p.M, m, n)) = a8_pack4(v[0], v[1], v[2], v[3], a8_inverse(eb));
+        if ((tx & 7) == 0) e.e[a8_scale_at(p.M, m, n)] = (uint8_t)eb;
       }
     }
     act_values<4>(e.act, v);

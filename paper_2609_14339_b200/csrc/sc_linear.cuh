@@ -17,7 +17,7 @@ struct LinEpilogue {
   const void* res;          // forward: same type as out, or null
   int8_t* q;                // forward: written; input: read; or null
   uint8_t* e;
-  int64_t wide;             // row stride of q (e: wide / 32)
+  int64_t wide;             // columns of D rounded up to 32; the checkpoint's tokens are the rows of D
   int64_t ldo, ldr;
   int out_f32;
   int act;

@@ -91,14 +91,14 @@ __device__ __forceinline__ void epilogue_row32(const LinEpilogue& e, const LtSha
       for (int j = 0; j < 32; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
       const uint32_t eb = a8_scale_byte(top);
       const float inv = a8_inverse(eb);
-      uint4* q = reinterpret_cast<uint4*>(e.q + row * e.wide + col);
+      uint4* q = reinterpret_cast<uint4*>(e.q + a8_at(sh.M, row, col));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const float* x = v + 16 * h;
         q[h] = make_uint4(a8_pack4(x[0], x[1], x[2], x[3], inv), a8_pack4(x[4], x[5], x[6], x[7], inv),
                           a8_pack4(x[8], x[9], x[10], x[11], inv), a8_pack4(x[12], x[13], x[14], x[15], inv));
       }
-      e.e[row * (e.wide / 32) + col / 32] = (uint8_t)eb;
+      e.e[a8_scale_at(sh.M, row, col)] = (uint8_t)eb;
     }
     act_values<32>(e.act, v);
     if (e.res) {
@@ -126,9 +126,9 @@ __device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtSha
 #pragma unroll
     for (int j = 0; j < 32; j += 8) load8(e.res, e.out_f32, row * e.ldr + col + j, sh.vec, left - j, aux + j);
   } else if (KIND == kEpiInput && e.q) {
-    const uint4* q = reinterpret_cast<const uint4*>(e.q + row * e.wide + col);
+    const uint4* q = reinterpret_cast<const uint4*>(e.q + a8_at(sh.M, row, col));
     const uint4 a = q[0], b = q[1];
-    const float step = a8_step(e.e[row * (e.wide / 32) + col / 32]);
+    const float step = a8_step(e.e[a8_scale_at(sh.M, row, col)]);
     a8_unpack4(a.x, step, aux); a8_unpack4(a.y, step, aux + 4); a8_unpack4(a.z, step, aux + 8); a8_unpack4(a.w, step, aux + 12);
     a8_unpack4(b.x, step, aux + 16); a8_unpack4(b.y, step, aux + 20); a8_unpack4(b.z, step, aux + 24); a8_unpack4(b.w, step, aux + 28);
     act_slopes<32>(e.act, aux);
@@ -391,23 +391,24 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 // ---------------------------------------------------------------------------------------- split contraction
 // One column of D (a lane of the accumulator) per thread, `count` rows of D at a time.
 template <int KIND, int CNT>
-__device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtShape& sh, float* v, int64_t row0, int col,
-                                                 float bias, int lane) {
+__device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtShape& sh, float* v, int64_t row0, int64_t rows_end,
+                                                 int col, float bias, int lane) {
   const bool inside = col < sh.N;
+  const int64_t tokens = sh.M;
   float aux[CNT];
   if (KIND == kEpiForward && e.res) {
 #pragma unroll
     for (int j = 0; j < CNT; ++j) {
       const int64_t i = (row0 + j) * e.ldr + col;
-      aux[j] = !(inside && row0 + j < sh.M) ? 0.f
+      aux[j] = !(inside && row0 + j < rows_end) ? 0.f
                : e.out_f32                  ? static_cast<const float*>(e.res)[i]
                                             : __bfloat162float(static_cast<const bf16*>(e.res)[i]);
     }
   } else if (KIND == kEpiInput && e.q) {
 #pragma unroll
     for (int j = 0; j < CNT; ++j) {
-      const bool ok = inside && row0 + j < sh.M;
-      aux[j] = ok ? (float)e.q[(row0 + j) * e.wide + col] * a8_step(e.e[(row0 + j) * (e.wide / 32) + col / 32]) : 0.f;
+      const bool ok = inside && row0 + j < rows_end;
+      aux[j] = ok ? (float)e.q[a8_at(tokens, row0 + j, col)] * a8_step(e.e[a8_scale_at(tokens, row0 + j, col)]) : 0.f;
     }
     act_slopes<CNT>(e.act, aux);
   }
@@ -419,9 +420,9 @@ __device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtS
       for (int j = 0; j < CNT; ++j) {
         const uint32_t eb = a8_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[j]) & 0x7fffffffu));
         const float inv = a8_inverse(eb);
-        if (row0 + j < sh.M && col < e.wide) {
-          e.q[(row0 + j) * e.wide + col] = (int8_t)(inv == 0.f ? 0u : a8_round(v[j], inv) & 255u);
-          if (lane == 0) e.e[(row0 + j) * (e.wide / 32) + col / 32] = (uint8_t)eb;
+        if (row0 + j < rows_end && col < e.wide) {
+          e.q[a8_at(tokens, row0 + j, col)] = (int8_t)(inv == 0.f ? 0u : a8_round(v[j], inv) & 255u);
+          if (lane == 0) e.e[a8_scale_at(tokens, row0 + j, col)] = (uint8_t)eb;
         }
       }
     }
@@ -442,7 +443,7 @@ __device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtS
   if (inside) {
 #pragma unroll
     for (int j = 0; j < CNT; ++j) {
-      if (row0 + j < sh.M) {
+      if (row0 + j < rows_end) {
         const int64_t i = (row0 + j) * e.ldo + col;
         if (e.out_f32) static_cast<float*>(e.out)[i] = v[j];
         else static_cast<bf16*>(e.out)[i] = __float2bfloat16_rn(v[j]);
@@ -553,7 +554,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
         float v[16];
         tmem_ld16(d + c, v);
         tmem_ld_wait();
-        epilogue_columns<KIND, 16>(epi, sh, v, row0 + c, col, bias, lane);
+        epilogue_columns<KIND, 16>(epi, sh, v, row0 + c, sh.M, col, bias, lane);
         __syncwarp();
       }
     }
@@ -590,10 +591,8 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
         for (int s = 0; s < 8; ++s)
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] += w[s][j];
-        // the rows past this block's share belong to the next block: give them a row outside D
-        LtShape mine_sh = sh;
-        mine_sh.M = row0 + last < sh.M ? (int)(row0 + last) : sh.M;
-        epilogue_columns<KIND, 4>(epi, mine_sh, v, row0 + c, col, bias, lane);
+        // the rows past this block's share belong to the next block
+        epilogue_columns<KIND, 4>(epi, sh, v, row0 + c, row0 + last < sh.M ? row0 + last : sh.M, col, bias, lane);
       }
     }
     __syncwarp();

@@ -287,8 +287,8 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
           if (c < wide) {
 #pragma unroll
             for (int i = 0; i < EPT; i += 4)
-              *reinterpret_cast<uint32_t*>(q + r * wide + c + i) = a8_pack4(y[i], y[i + 1], y[i + 2], y[i + 3], inv);
-            if (threadIdx.x % (32 / EPT) == 0) qe[r * (wide / 32) + c / 32] = (uint8_t)e;
+              *reinterpret_cast<uint32_t*>(q + a8_at(rows, r, c + i)) = a8_pack4(y[i], y[i + 1], y[i + 2], y[i + 3], inv);
+            if (threadIdx.x % (32 / EPT) == 0) qe[a8_scale_at(rows, r, c)] = (uint8_t)e;
           }
         } else {
 #pragma unroll
@@ -297,8 +297,8 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
             const float inv = a8_inverse(e);
             const int c = P::col(i);
             if (c < wide) {
-              q[r * wide + c] = (int8_t)(inv == 0.f ? 0u : a8_round(y[i], inv) & 255u);
-              if ((threadIdx.x & 31) == 0) qe[r * (wide / 32) + c / 32] = (uint8_t)e;
+              q[a8_at(rows, r, c)] = (int8_t)(inv == 0.f ? 0u : a8_round(y[i], inv) & 255u);
+              if ((threadIdx.x & 31) == 0) qe[a8_scale_at(rows, r, c)] = (uint8_t)e;
             }
           }
         }
@@ -419,8 +419,8 @@ norm_forward_wide_kernel(const void* X, const float* __restrict__ weight, const 
       if (q) {
         const uint32_t e = a8_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(y) & 0x7fffffffu));
         const float inv = a8_inverse(e);
-        q[r * wide + c] = (int8_t)(inv == 0.f ? 0u : a8_round(y, inv) & 255u);
-        if ((threadIdx.x & 31) == 0) qe[r * (wide / 32) + c / 32] = (uint8_t)e;
+        q[a8_at(rows, r, c)] = (int8_t)(inv == 0.f ? 0u : a8_round(y, inv) & 255u);
+        if ((threadIdx.x & 31) == 0) qe[a8_scale_at(rows, r, c)] = (uint8_t)e;
       }
       if (c < cols) st1<F32>(Y, r * ldy + c, y);
     }
@@ -536,8 +536,15 @@ struct Forward {
 template <bool F32, int EPT, bool VEC, int THREADS>
 void forward_launch(const Forward& f, cudaStream_t s) {
   const int smem = 2 * (int)sizeof(Params<EPT, THREADS>);
-  if (smem > 40 * 1024)
-    cudaFuncSetAttribute(norm_forward_kernel<F32, EPT, VEC, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (smem > 40 * 1024) {          // once per device: the call costs as much as a launch
+    static std::atomic<uint64_t> raised{0};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!(raised.load(std::memory_order_relaxed) >> (dev & 63) & 1)) {
+      cudaFuncSetAttribute(norm_forward_kernel<F32, EPT, VEC, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      raised.fetch_or(1ull << (dev & 63), std::memory_order_relaxed);
+    }
+  }
   const int64_t most = (int64_t)kNormSms * blocks_per_sm(THREADS, 1024), groups = EPT == 16 ? f.rows : (f.rows + 1) / 2;
   norm_forward_kernel<F32, EPT, VEC, THREADS><<<(unsigned)(groups < most ? groups : most), THREADS, smem, s>>>(
       f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e, f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);

@@ -10,6 +10,8 @@ property of a tensor once and the stream's handle is taken without building a St
 """
 from __future__ import annotations
 
+from functools import lru_cache
+
 import torch
 
 from .binding import (SC_ACT_GELU, SC_ACT_NONE, SC_ACT_RELU, SC_ACT_SILU, SC_DTYPE_BF16, SC_DTYPE_FP32, SCError,
@@ -20,42 +22,17 @@ _DTYPES = {torch.bfloat16: SC_DTYPE_BF16, torch.float32: SC_DTYPE_FP32}
 _F32, _U8 = torch.float32, torch.uint8
 
 
-class _Elsewhere:
-    """Makes a given stream (and its device) current for the allocations and the launch of one call."""
-
-    def __init__(self, device: int, stream):
-        if stream is not None:
-            if stream.device.index != device:
-                raise ValueError("stream is on device %d, the tensors are on device %d" % (stream.device.index, device))
-            self._guard = torch.cuda.stream(stream)
-        else:
-            self._guard = torch.cuda.device(device)
-
-    def __enter__(self):
-        self._guard.__enter__()
-
-    def __exit__(self, *exc):
-        self._guard.__exit__(*exc)
-
-
-class _Here:
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *exc):
-        pass
-
-
-_HERE = _Here()
-
-
 def _on(device: int, stream):
-    if stream is None and torch._C._cuda_getDevice() == device:
-        return _HERE
-    return _Elsewhere(device, stream)
+    """Makes a stream (and its device) current for one call: its allocations come from that stream's pool."""
+    if stream is None:
+        return torch.cuda.device(device)
+    if stream.device.index != device:
+        raise ValueError("stream is on device %d, the tensors are on device %d" % (stream.device.index, device))
+    return torch.cuda.stream(stream)
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_device = torch._C._cuda_getDevice
 
 
 def _act(act) -> int:
@@ -96,7 +73,7 @@ def _matrix(name, t, rows=None, cols=None, dtype=None, device=None):
 def _vector(name, t, n, device):
     if t is None:
         return None
-    if not t.is_cuda or t.get_device() != device or t.dtype is not _F32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+    if not t.is_cuda or t.get_device() != device or t.dtype is not _F32 or t.numel() != n or t.dim() != 1 or not t.is_contiguous():
         raise ValueError("%s must be a contiguous float32 tensor of shape (%d,) on device %d" % (name, n, device))
     return t.data_ptr()
 
@@ -128,6 +105,27 @@ def _out_dtype(out, out_dtype, default):
     return dt
 
 
+@lru_cache(maxsize=4096)
+def _act8_bytes(tokens: int, features: int) -> int:
+    need = load_library().sc_act8_bytes(tokens, features)
+    if need == 0:
+        raise SCError(-2, "sc_act8_bytes")
+    return int(need)
+
+
+@lru_cache(maxsize=4096)
+def _norm_bytes(rows: int, cols: int) -> int:
+    return int(load_library().sc_layernorm_workspace_bytes(rows, cols))
+
+
+@lru_cache(maxsize=4096)
+def _weight_grad_bytes(dtype: int, tokens: int, rows: int, cols: int) -> int:
+    need = load_library().sc_linear_weight_grad_workspace_bytes(dtype, tokens, rows, cols)
+    if need == 0:
+        raise SCError(-2, "sc_linear_weight_grad_workspace_bytes")
+    return int(need)
+
+
 class Act8:
     """An activation kept in 8 bits: blocks of 32 features share a power of two (33 bytes for 32 values)."""
 
@@ -151,10 +149,7 @@ class Act8:
 
     @staticmethod
     def nbytes(tokens: int, features: int) -> int:
-        need = load_library().sc_act8_bytes(int(tokens), int(features))
-        if need == 0:
-            raise SCError(-2, "sc_act8_bytes")
-        return int(need)
+        return _act8_bytes(int(tokens), int(features))
 
 
 def _saved(name, saved, tokens, features, device):
@@ -171,18 +166,20 @@ def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, save=None, out=None
     what layer_norm_backward takes. save: an Act8 of X's shape that receives Y in 8 bits. out may be X."""
     rows, cols, ldx = _matrix("X", X)
     dev, dt = X.get_device(), X.dtype
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return layer_norm(X, weight, bias, eps, save, out, stats)
     w, b = _vector("weight", weight, cols, dev), _vector("bias", bias, cols, dev)
     a8 = None if save is None else _saved("save", save, rows, cols, dev)
-    with _on(dev, stream):
-        if out is None:
-            out, ldy = X.new_empty((rows, cols)), cols
-        else:
-            ldy = _matrix("out", out, rows, cols, dt, dev)[2]
-        if stats is None:
-            stats = X.new_empty((2, rows), dtype=_F32)
-        _done(load_library().sc_layernorm_forward(X.data_ptr(), _DTYPES[dt], w, b, eps, out.data_ptr(),
-                                                  _stats(stats, rows, dev), a8, rows, cols, ldx, ldy, _raw_stream(dev)),
-              "sc_layernorm_forward")
+    if out is None:
+        out, ldy = X.new_empty((rows, cols)), cols
+    else:
+        ldy = _matrix("out", out, rows, cols, dt, dev)[2]
+    if stats is None:
+        stats = X.new_empty((2, rows), dtype=_F32)
+    _done(load_library().sc_layernorm_forward(X.data_ptr(), _DTYPES[dt], w, b, eps, out.data_ptr(),
+                                              _stats(stats, rows, dev), a8, rows, cols, ldx, ldy, _raw_stream(dev)),
+          "sc_layernorm_forward")
     return out, stats
 
 
@@ -192,6 +189,9 @@ def layer_norm_backward(dY, X, weight, stats, residual_grad=None, out=None, dwei
     out may be dY or residual_grad. workspace: uint8, sc_layernorm_workspace_bytes(rows, cols)."""
     rows, cols, ldx = _matrix("X", X)
     dev, dt = X.get_device(), X.dtype
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return layer_norm_backward(dY, X, weight, stats, residual_grad, out, dweight, dbias, workspace)
     lddy = _matrix("dY", dY, rows, cols, dt, dev)[2]
     r, ldr = None, 0
     if residual_grad is not None:
@@ -199,22 +199,21 @@ def layer_norm_backward(dY, X, weight, stats, residual_grad=None, out=None, dwei
         r = residual_grad.data_ptr()
     w, st = _vector("weight", weight, cols, dev), _stats(stats, rows, dev)
     lib = load_library()
-    need = lib.sc_layernorm_workspace_bytes(rows, cols)
-    with _on(dev, stream):
-        if out is None:
-            out, lddx = X.new_empty((rows, cols)), cols
-        else:
-            lddx = _matrix("out", out, rows, cols, dt, dev)[2]
-        if dweight is None:
-            dweight = stats.new_empty((cols,))
-        if dbias is None:
-            dbias = stats.new_empty((cols,))
-        if workspace is None:
-            workspace = X.new_empty((need,), dtype=_U8)
-        _done(lib.sc_layernorm_backward(dY.data_ptr(), X.data_ptr(), _DTYPES[dt], w, st, r, out.data_ptr(),
-                                        _vector("dweight", dweight, cols, dev), _vector("dbias", dbias, cols, dev), rows,
-                                        cols, lddy, ldx, ldr, lddx, _buffer("workspace", workspace, need, dev),
-                                        workspace.numel(), _raw_stream(dev)), "sc_layernorm_backward")
+    need = _norm_bytes(rows, cols)
+    if out is None:
+        out, lddx = X.new_empty((rows, cols)), cols
+    else:
+        lddx = _matrix("out", out, rows, cols, dt, dev)[2]
+    if dweight is None:
+        dweight = stats.new_empty((cols,))
+    if dbias is None:
+        dbias = stats.new_empty((cols,))
+    if workspace is None:
+        workspace = X.new_empty((need,), dtype=_U8)
+    _done(lib.sc_layernorm_backward(dY.data_ptr(), X.data_ptr(), _DTYPES[dt], w, st, r, out.data_ptr(),
+                                    _vector("dweight", dweight, cols, dev), _vector("dbias", dbias, cols, dev), rows,
+                                    cols, lddy, ldx, ldr, lddx, _buffer("workspace", workspace, need, dev),
+                                    workspace.numel(), _raw_stream(dev)), "sc_layernorm_backward")
     return out, dweight, dbias
 
 
@@ -222,11 +221,13 @@ def act8_compress(X, out=None, stream=None) -> Act8:
     """X (bf16 or fp32) as an 8-bit checkpoint."""
     tokens, features, ldx = _matrix("X", X)
     dev = X.get_device()
-    with _on(dev, stream):
-        if out is None:
-            out = Act8._new(tokens, features, X.new_empty((Act8.nbytes(tokens, features),), dtype=_U8))
-        _done(load_library().sc_act8_compress(X.data_ptr(), _DTYPES[X.dtype], _saved("out", out, tokens, features, dev),
-                                              tokens, features, ldx, _raw_stream(dev)), "sc_act8_compress")
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return act8_compress(X, out)
+    if out is None:
+        out = Act8._new(tokens, features, X.new_empty((_act8_bytes(tokens, features),), dtype=_U8))
+    _done(load_library().sc_act8_compress(X.data_ptr(), _DTYPES[X.dtype], _saved("out", out, tokens, features, dev),
+                                          tokens, features, ldx, _raw_stream(dev)), "sc_act8_compress")
     return out
 
 
@@ -237,12 +238,14 @@ def act8_expand(saved, act="none", out=None, out_dtype=torch.bfloat16, stream=No
         raise ValueError("saved must be an Act8")
     tokens, features, data = saved.tokens, saved.features, saved.data
     dev = data.get_device()
-    with _on(dev, stream):
-        if out is None:
-            out = data.new_empty((tokens, features), dtype=_out_dtype(None, out_dtype, None))
-        ldy = _matrix("out", out, tokens, features, None, dev)[2]
-        _done(load_library().sc_act8_expand(data.data_ptr(), a, out.data_ptr(), _DTYPES[out.dtype], tokens, features, ldy,
-                                            _raw_stream(dev)), "sc_act8_expand")
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return act8_expand(saved, act, out, out_dtype)
+    if out is None:
+        out = data.new_empty((tokens, features), dtype=_out_dtype(None, out_dtype, None))
+    ldy = _matrix("out", out, tokens, features, None, dev)[2]
+    _done(load_library().sc_act8_expand(data.data_ptr(), a, out.data_ptr(), _DTYPES[out.dtype], tokens, features, ldy,
+                                        _raw_stream(dev)), "sc_act8_expand")
     return out
 
 
@@ -251,13 +254,15 @@ def act8_backward(dA, saved, act, out=None, stream=None):
     a = _act(act)
     tokens, features, ldda = _matrix("dA", dA)
     dev, dt = dA.get_device(), dA.dtype
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return act8_backward(dA, saved, act, out)
     a8 = _saved("saved", saved, tokens, features, dev)
-    with _on(dev, stream):
-        if out is None:
-            out = dA.new_empty((tokens, features))
-        lddz = _matrix("out", out, tokens, features, dt, dev)[2]
-        _done(load_library().sc_act8_backward(dA.data_ptr(), a8, a, out.data_ptr(), _DTYPES[dt], tokens, features, ldda,
-                                              lddz, _raw_stream(dev)), "sc_act8_backward")
+    if out is None:
+        out = dA.new_empty((tokens, features))
+    lddz = _matrix("out", out, tokens, features, dt, dev)[2]
+    _done(load_library().sc_act8_backward(dA.data_ptr(), a8, a, out.data_ptr(), _DTYPES[dt], tokens, features, ldda,
+                                          lddz, _raw_stream(dev)), "sc_act8_backward")
     return out
 
 
@@ -268,6 +273,9 @@ def linear(X, W, bias=None, residual=None, act="none", save=None, out=None, out_
     a = _act(act)
     tokens, cols, ldx = _matrix("X", X)
     dev, dt = X.get_device(), X.dtype
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return linear(X, W, bias, residual, act, save, out, out_dtype, status)
     rows, _, ldw = _matrix("W", W, None, cols, dt, dev)
     odt = _out_dtype(out, out_dtype, dt)
     r, ldr = None, 0
@@ -276,14 +284,13 @@ def linear(X, W, bias=None, residual=None, act="none", save=None, out=None, out_
         r = residual.data_ptr()
     b = _vector("bias", bias, rows, dev)
     a8 = None if save is None else _saved("save", save, tokens, rows, dev)
-    with _on(dev, stream):
-        if out is None:
-            out, ldy = X.new_empty((tokens, rows), dtype=odt), rows
-        else:
-            ldy = _matrix("out", out, tokens, rows, None, dev)[2]
-        _done(load_library().sc_linear_forward(X.data_ptr(), W.data_ptr(), _DTYPES[dt], b, r, out.data_ptr(), _DTYPES[odt],
-                                               a, a8, tokens, rows, cols, ldx, ldw, ldr, ldy, _status(status, dev),
-                                               _raw_stream(dev)), "sc_linear_forward")
+    if out is None:
+        out, ldy = X.new_empty((tokens, rows), dtype=odt), rows
+    else:
+        ldy = _matrix("out", out, tokens, rows, None, dev)[2]
+    _done(load_library().sc_linear_forward(X.data_ptr(), W.data_ptr(), _DTYPES[dt], b, r, out.data_ptr(), _DTYPES[odt],
+                                           a, a8, tokens, rows, cols, ldx, ldw, ldr, ldy, _status(status, dev),
+                                           _raw_stream(dev)), "sc_linear_forward")
     return out
 
 
@@ -293,17 +300,19 @@ def linear_backward_input(dY, W, saved=None, act="none", out=None, out_dtype=Non
     a = _act(act)
     tokens, rows, lddy = _matrix("dY", dY)
     dev, dt = dY.get_device(), dY.dtype
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return linear_backward_input(dY, W, saved, act, out, out_dtype, status)
     _, cols, ldw = _matrix("W", W, rows, None, dt, dev)
     odt = _out_dtype(out, out_dtype, dt)
     a8 = None if saved is None else _saved("saved", saved, tokens, cols, dev)
-    with _on(dev, stream):
-        if out is None:
-            out, lddx = dY.new_empty((tokens, cols), dtype=odt), cols
-        else:
-            lddx = _matrix("out", out, tokens, cols, None, dev)[2]
-        _done(load_library().sc_linear_backward_input(dY.data_ptr(), W.data_ptr(), _DTYPES[dt], a8, a, out.data_ptr(),
-                                                      _DTYPES[odt], tokens, rows, cols, lddy, ldw, lddx,
-                                                      _status(status, dev), _raw_stream(dev)), "sc_linear_backward_input")
+    if out is None:
+        out, lddx = dY.new_empty((tokens, cols), dtype=odt), cols
+    else:
+        lddx = _matrix("out", out, tokens, cols, None, dev)[2]
+    _done(load_library().sc_linear_backward_input(dY.data_ptr(), W.data_ptr(), _DTYPES[dt], a8, a, out.data_ptr(),
+                                                  _DTYPES[odt], tokens, rows, cols, lddy, ldw, lddx,
+                                                  _status(status, dev), _raw_stream(dev)), "sc_linear_backward_input")
     return out
 
 
@@ -315,26 +324,26 @@ def linear_weight_grad(dY, saved, act="none", scale: float = 1.0, out=None, out_
     a = _act(act)
     tokens, rows, lddy = _matrix("dY", dY)
     dev, dt = dY.get_device(), dY.dtype
+    if stream is not None or _device() != dev:
+        with _on(dev, stream):
+            return linear_weight_grad(dY, saved, act, scale, out, out_dtype, dbias, workspace, status)
     if not isinstance(saved, Act8):
         raise ValueError("saved must be an Act8")
     cols = saved.features
     a8 = _saved("saved", saved, tokens, cols, dev)
     odt = _out_dtype(out, out_dtype, dt)
     lib = load_library()
-    need = lib.sc_linear_weight_grad_workspace_bytes(_DTYPES[dt], tokens, rows, cols)
-    if need == 0:
-        raise SCError(-2, "sc_linear_weight_grad_workspace_bytes")
-    with _on(dev, stream):
-        if out is None:
-            out = dY.new_empty((rows, cols), dtype=odt)
-        elif _matrix("out", out, rows, cols, None, dev)[2] != cols:
-            raise ValueError("out must be contiguous")
-        if dbias is None:
-            dbias = dY.new_empty((rows,), dtype=_F32)
-        if workspace is None:
-            workspace = dY.new_empty((need,), dtype=_U8)
-        _done(lib.sc_linear_weight_grad(dY.data_ptr(), _DTYPES[dt], a8, a, scale, out.data_ptr(), _DTYPES[odt],
-                                        _vector("dbias", dbias, rows, dev), tokens, rows, cols, lddy,
-                                        _buffer("workspace", workspace, need, dev), workspace.numel(),
-                                        _status(status, dev), _raw_stream(dev)), "sc_linear_weight_grad")
+    need = _weight_grad_bytes(_DTYPES[dt], tokens, rows, cols)
+    if out is None:
+        out = dY.new_empty((rows, cols), dtype=odt)
+    elif _matrix("out", out, rows, cols, None, dev)[2] != cols:
+        raise ValueError("out must be contiguous")
+    if dbias is None:
+        dbias = dY.new_empty((rows,), dtype=_F32)
+    if workspace is None:
+        workspace = dY.new_empty((need,), dtype=_U8)
+    _done(lib.sc_linear_weight_grad(dY.data_ptr(), _DTYPES[dt], a8, a, scale, out.data_ptr(), _DTYPES[odt],
+                                    _vector("dbias", dbias, rows, dev), tokens, rows, cols, lddy,
+                                    _buffer("workspace", workspace, need, dev), workspace.numel(),
+                                    _status(status, dev), _raw_stream(dev)), "sc_linear_weight_grad")
     return out, dbias
