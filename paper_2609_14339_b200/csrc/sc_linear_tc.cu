@@ -781,13 +781,19 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
       return split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, sh, epi, split, status)
                        : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, sh, epi, 1, status);
     };
-    // The last wave of a launch that needs more than one is seldom full. Where every one of its tiles can have two to four
-    // pairs, it becomes a launch of its own with the contraction split, which starts on the SMs the full waves leave
-    // (4096 x 4096 x 14336, 256 tiles on 74 pairs: 3.5 waves instead of 4).
+    // The last wave of a launch that needs more than one is seldom full. It becomes a launch of its own with the contraction
+    // split over two to four pairs a tile, which starts on the SMs the full waves leave, where the rounds that takes are
+    // shorter than the wave (in stages of 64; a round's start and join cost about 13 of them). 4096 x 4096 x 14336, 256
+    // tiles on 74 pairs: two rounds of a third instead of a fourth wave; 4096 x 14336 x 4096, 896 tiles: one of a quarter.
     const int64_t full = tiles / slots * slots, rest = tiles - full;
     int rest_split = 1;
-    if (c.split == 1 && full > 0 && rest > 0)
-      for (int k = 2; k <= 4 && rest <= dev->clusters[k] && sh.kchunks >= 16 * k; ++k) rest_split = k;
+    if (c.split == 1 && full > 0 && rest > 0) {
+      int64_t best = sh.kchunks - 8;
+      for (int k = 2; k <= 4; ++k) {
+        const int64_t cost = up(rest, dev->clusters[k]) * (up(sh.kchunks, k) + 13);
+        if (cost < best) { best = cost; rest_split = k; }
+      }
+    }
     if (rest_split > 1) {
       if (go(0, full, 1, false) != cudaSuccess || go(full, tiles, rest_split, true) != cudaSuccess) return SC_ERR_CUDA;
     } else if (go(0, tiles, c.split, false) != cudaSuccess) {
