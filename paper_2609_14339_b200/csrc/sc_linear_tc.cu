@@ -48,7 +48,8 @@ struct LtBars {
   uint32_t tmem_slot;
   int abort_flag;
   int never_flag;
-  float red[8][32];              // column sums of dY, one row per epilogue warp
+  float red[8][128];             // column sums of dY, one row per epilogue warp
+  float db_part[128];            // split contraction: this block's share of them
 };
 
 template <int KIND>
@@ -137,58 +138,79 @@ __device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtSha
 
 // ---------------------------------------------------------------------------------------- bias gradient
 // The weight gradient's epilogue warps have nothing to do until the first tile is finished: they sum dY's columns
-// meanwhile, 8 * G columns per block and turn, the tokens over the threads, joined in a fixed order. dY comes out of L2 for
-// the most part (the pipeline reads it too) and no launch, workspace or second pass is spent on it. G is the widest that
-// still gives every block columns of its own: with 32 columns everywhere, 1024 x 16384 tokens kept 32 of 96 blocks busy
-// for 64 us.
+// meanwhile, out of L2 for the most part (the pipeline reads it too); no launch, workspace or second pass is spent on it.
+//
+// Sums of columns c0 .. c0 + 8 G - 1 over tokens t0 .. t1 - 1 to out: the tokens over the threads, joined in a fixed order.
 template <int WARPS, int G>
-__device__ __forceinline__ void bias_gradient_by(const LinEpilogue& e, int rows, float (*red)[32]) {
+__device__ __forceinline__ void column_sums(const LinEpilogue& e, int64_t rows, int64_t c0, int64_t t0, int64_t t1, float (*red)[128],
+                                            float* out) {
   constexpr int LANES = WARPS * 32 / G, UNROLL = 8;            // tokens side by side; tokens per thread and turn
   const int tid = threadIdx.x - 64, warp = tid >> 5, lane = tid & 31, group = tid % G;
   const bf16* dy = static_cast<const bf16*>(e.dy);
-  for (int64_t c0 = (int64_t)blockIdx.x * 8 * G; c0 < rows; c0 += (int64_t)gridDim.x * 8 * G) {
-    const int64_t c = c0 + group * 8;
-    float s[8] = {};
-    if (c + 8 <= rows) {
-      for (int64_t t = tid / G; t < e.tokens; t += LANES * UNROLL) {
-        uint4 x[UNROLL];
+  const int64_t c = c0 + group * 8;
+  float s[8] = {};
+  if (c + 8 <= rows) {
+    for (int64_t t = t0 + tid / G; t < t1; t += LANES * UNROLL) {
+      uint4 x[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u)
-          x[u] = t + u * LANES < e.tokens ? *reinterpret_cast<const uint4*>(dy + (t + u * LANES) * e.ld_dy + c) : make_uint4(0u, 0u, 0u, 0u);
+      for (int u = 0; u < UNROLL; ++u)
+        x[u] = t + u * LANES < t1 ? *reinterpret_cast<const uint4*>(dy + (t + u * LANES) * e.ld_dy + c) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-          const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      for (int u = 0; u < UNROLL; ++u) {
+        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) { s[2 * j] += __uint_as_float(w[j] << 16); s[2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u); }
-        }
+        for (int j = 0; j < 4; ++j) { s[2 * j] += __uint_as_float(w[j] << 16); s[2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u); }
       }
-    } else {
-      for (int64_t t = tid / G; t < e.tokens; t += LANES)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < rows) s[j] += __bfloat162float(dy[t * e.ld_dy + c + j]);
     }
+  } else {
+    for (int64_t t = t0 + tid / G; t < t1; t += LANES)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 8; ++j)
+        if (c + j < rows) s[j] += __bfloat162float(dy[t * e.ld_dy + c + j]);
+  }
 #pragma unroll
-      for (int o = G; o < 32; o <<= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
-    if (lane < G)
+  for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) red[warp][lane * 8 + j] = s[j];
-    asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
-    if (warp == 0 && lane < 8 * G && c0 + lane < rows) {
-      float v = 0.f;
+    for (int o = G; o < 32; o <<= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+  if (lane < G)
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) v += red[w][lane];
-      e.db[c0 + lane] = v;
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
+    for (int j = 0; j < 8; ++j) red[warp][lane * 8 + j] = s[j];
+  asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
+  if (tid < 8 * G && c0 + tid < rows) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) v += red[w][tid];
+    out[tid] = v;
+  }
+  asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory");
+}
+// Every block columns of its own over all tokens, as wide as still gives every block some (8 G = 32 or 8).
+template <int WARPS>
+__device__ __forceinline__ void bias_gradient(const LinEpilogue& e, int rows, float (*red)[128]) {
+  const bool wide = rows >= 32 * (int)gridDim.x;
+  const int64_t step = wide ? 32 : 8;
+  for (int64_t c0 = blockIdx.x * step; c0 < rows; c0 += gridDim.x * step) {
+    if (wide) column_sums<WARPS, 4>(e, rows, c0, 0, e.tokens, red, e.db + c0);
+    else column_sums<WARPS, 1>(e, rows, c0, 0, e.tokens, red, e.db + c0);
   }
 }
-template <int WARPS>
-__device__ __forceinline__ void bias_gradient(const LinEpilogue& e, int rows, float (*red)[32]) {
-  if (rows >= 32 * (int)gridDim.x) bias_gradient_by<WARPS, 4>(e, rows, red);
-  else bias_gradient_by<WARPS, 1>(e, rows, red);
+// Split contraction: a block sums its own share of the tokens, of its tile's 128 columns of dY the part that falls to its
+// tile column (the tiles beside it have the same 128); joined with the products' sums. Over all tokens instead, a block's
+// columns took longer than its share of the product (1024 x 520 over 16384 tokens: 45 us, 33 us without a bias gradient).
+__device__ __forceinline__ int bias_share(int tiles_n) {        // groups of 8 columns per tile column, a power of two
+  int g = 1;
+  while (g < 16 && g * tiles_n < 16) g *= 2;
+  return g;
+}
+__device__ __forceinline__ void bias_gradient_part(const LinEpilogue& e, int rows, int64_t c0, int g, int64_t t0, int64_t t1,
+                                                   float (*red)[128], float* out) {
+  switch (g) {
+    case 1: column_sums<8, 1>(e, rows, c0, t0, t1, red, out); break;
+    case 2: column_sums<8, 2>(e, rows, c0, t0, t1, red, out); break;
+    case 4: column_sums<8, 4>(e, rows, c0, t0, t1, red, out); break;
+    case 8: column_sums<8, 8>(e, rows, c0, t0, t1, red, out); break;
+    default: column_sums<8, 16>(e, rows, c0, t0, t1, red, out);
+  }
 }
 
 // ---------------------------------------------------------------------------------------- two SMs per 256 x bn tile
@@ -310,7 +332,18 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     __syncwarp();
   } else {
     uint32_t t = 0;
-    if (KIND == kEpiWeight && epi.db) bias_gradient<8>(epi, sh.M, bars->red);
+    if (KIND == kEpiWeight && epi.db) {
+      if (!SPLIT) {
+        bias_gradient<8>(epi, sh.M, bars->red);
+      } else {
+        const int tm = sh.m_fastest ? pair % sh.tiles_m : pair / sh.tiles_n, tn = sh.m_fastest ? pair / sh.tiles_m : pair % sh.tiles_n;
+        const int g = bias_share(sh.tiles_n);
+        const int64_t t0 = (int64_t)k_begin * kLtK, t1 = (int64_t)k_end * kLtK;
+        if (tn * g < 16)
+          bias_gradient_part(epi, sh.M, tm * 256 + (int)rank * 128 + tn * g * 8, g, t0, t1 < epi.tokens ? t1 : epi.tokens, bars->red,
+                             bars->db_part);
+      }
+    }
     for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
       const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
       const uint32_t ab = t & 1;
@@ -355,6 +388,15 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     cluster_sync_all();
     if (warp >= 2) {
       const int tm = sh.m_fastest ? pair % sh.tiles_m : pair / sh.tiles_n, tn = sh.m_fastest ? pair / sh.tiles_m : pair % sh.tiles_n;
+      if (KIND == kEpiWeight && epi.db && part_k == 0) {
+        const int g = bias_share(sh.tiles_n), c = threadIdx.x - 64;
+        const int64_t col = tm * 256 + (int)rank * 128 + tn * g * 8 + c;
+        if (tn * g < 16 && c < 8 * g && col < sh.M) {
+          float v = 0.f;
+          for (int s = 0; s < split; ++s) v += ld_shared_cluster(map_to_rank(smem_u32(&bars->db_part[c]), 2 * s + rank));
+          epi.db[col] = v;
+        }
+      }
       const int row = tm * 256 + (int)rank * 128 + q * 32 + lane, blocks = sh.bn / 32;
       const int last = blocks * (part_k + 1) / split;
       for (int blk = blocks * part_k / split + part; blk < last; blk += 2) {
