@@ -26,6 +26,7 @@ constexpr int kLtK = 64;                       // contraction per pipeline stage
 constexpr int kLtBox = 64 * kLtK * 2;          // one 64 x 64 bf16 box: 8 KB
 constexpr int kLtPairStages = 6;
 constexpr int kLtMaxStages = 8;
+constexpr int kLtStaging = 4096;              // per epilogue warp: two 32 x 32 bf16 blocks
 constexpr int kLtPairThreads = 320;            // producer, issuer, 8 epilogue warps
 constexpr int kLtSplitThreads = 192;           // producer, issuer, 4 epilogue warps
 
@@ -38,6 +39,7 @@ struct LtShape {
   int m_fastest;           // pair: which way consecutive tiles run
   int stages;              // split
   int vec;                 // out and res take 16-byte accesses
+  int staged;              // pair: bf16 out (and res) that TMA can describe; the epilogue goes through shared memory
   int vec_bias;
 };
 
@@ -48,7 +50,7 @@ struct LtBars {
   uint32_t tmem_slot;
   int abort_flag;
   int never_flag;
-  float red[8][128];             // column sums of dY, one row per epilogue warp
+  uint64_t res[8];               // pair: a residual block has landed, one per epilogue warp
   float db_part[128];            // split contraction: this block's share of them
 };
 
@@ -62,9 +64,10 @@ __device__ __forceinline__ uint64_t lt_desc(uint32_t saddr, bool mn, int k16) {
 }
 
 // ---------------------------------------------------------------------------------------- epilogue, one row per thread
-// 32 neighbouring columns (from a multiple of 32) of one row: v holds the sums
+// 32 neighbouring columns (from a multiple of 32) of one row: v holds the sums, then what is to be stored (forward:
+// without the residual)
 template <int KIND>
-__device__ __forceinline__ void epilogue_row32(const LinEpilogue& e, const LtShape& sh, const float* aux, float* v,
+__device__ __forceinline__ void epilogue_value32(const LinEpilogue& e, const LtShape& sh, const float* aux, float* v,
                                                int64_t row, int col) {
   const int left = sh.N - col;             // > 0
   if (KIND == kEpiForward) {
@@ -102,10 +105,6 @@ __device__ __forceinline__ void epilogue_row32(const LinEpilogue& e, const LtSha
       e.e[a8_scale_at(sh.M, row, col)] = (uint8_t)eb;
     }
     act_values<32>(e.act, v);
-    if (e.res) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] += aux[j];
-    }
   } else if (KIND == kEpiInput) {
     if (e.q) {
 #pragma unroll
@@ -115,18 +114,11 @@ __device__ __forceinline__ void epilogue_row32(const LinEpilogue& e, const LtSha
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] *= e.scale;
   }
-#pragma unroll
-  for (int j = 0; j < 32; j += 8)
-    if (j < left) store8(e.out, e.out_f32, row * e.ldo + col + j, sh.vec, left - j, v + j);
 }
-// what the epilogue needs besides the sums, read before the sums are waited for: residual, or slopes of the checkpoint
+// what the epilogue needs besides the sums, read before the sums are waited for: slopes of the checkpoint
 template <int KIND>
 __device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtShape& sh, float* aux, int64_t row, int col) {
-  const int left = sh.N - col;
-  if (KIND == kEpiForward && e.res) {
-#pragma unroll
-    for (int j = 0; j < 32; j += 8) load8(e.res, e.out_f32, row * e.ldr + col + j, sh.vec, left - j, aux + j);
-  } else if (KIND == kEpiInput && e.q) {
+  if (KIND == kEpiInput && e.q) {
     const uint4* q = reinterpret_cast<const uint4*>(e.q + a8_at(sh.M, row, col));
     const uint4 a = q[0], b = q[1];
     const float step = a8_step(e.e[a8_scale_at(sh.M, row, col)]);
@@ -134,6 +126,83 @@ __device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtSha
     a8_unpack4(b.x, step, aux + 16); a8_unpack4(b.y, step, aux + 20); a8_unpack4(b.z, step, aux + 24); a8_unpack4(b.w, step, aux + 28);
     act_slopes<32>(e.act, aux);
   }
+}
+
+// An epilogue warp's way out: blocks of 32 rows x 32 columns, a thread a row. Stored from the registers, a row's 64 bytes
+// are four pieces of 16, and the 4096 pieces of a block's 128 x 256 bf16 results took 6000 clocks, a quarter of a tile
+// with 2048 terms, the shared-memory pipe shared with the tensor core's operands meanwhile. So bf16 blocks go through two
+// 2 KB buffers per warp (64-byte swizzle: no two of 8 rows in one bank) and out by TMA, which cuts off what lies outside;
+// a residual comes in the same way, before the sums are waited for, and is added in place.
+struct WayOut {
+  uint8_t* buf;              // this warp's two buffers
+  uint64_t* bar;             // residual landed
+  uint32_t n;                // blocks so far: buffer n & 1, barrier phase n & 1
+};
+__device__ __forceinline__ uint4* staged_piece(uint8_t* buf, int row, int piece) {      // 16 bytes: 8 columns
+  return reinterpret_cast<uint4*>(buf + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+}
+// the residual of block n starts on its way; the store before the last, from the same buffer, has been read by then
+__device__ __forceinline__ void fetch_residual(WayOut& w, const CUtensorMap* map, int lane, int col, int row) {
+  if (lane == 0) {
+    tma_store_wait_read<1>();
+    mbar_expect_tx(w.bar, 2048);
+    tma_load_2d(w.buf + (w.n & 1) * 2048, map, w.bar, col, row);
+  }
+}
+// row0: the block's first row. Called by whole warps; false: a wait ran out.
+template <int KIND>
+__device__ __forceinline__ bool way_out(WayOut& w, const LinEpilogue& e, const LtShape& sh, const CUtensorMap* map_out, float* v,
+                                        int row0, int lane, int col, volatile int* abort_flag) {
+  const int row = row0 + lane, left = sh.N - col;
+  if (!sh.staged) {
+    if (row < sh.M && left > 0) {
+      if (KIND == kEpiForward && e.res) {
+        float r[8];
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+          load8(e.res, e.out_f32, (int64_t)row * e.ldr + col + j, sh.vec, left - j, r);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[j + i] += r[i];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 32; j += 8)
+        if (j < left) store8(e.out, e.out_f32, (int64_t)row * e.ldo + col + j, sh.vec, left - j, v + j);
+    }
+    return true;
+  }
+  uint8_t* buf = w.buf + (w.n & 1) * 2048;
+  if (KIND == kEpiForward && e.res) {
+    if (!mbar_wait(w.bar, w.n & 1, abort_flag)) return false;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const uint4 u = *staged_piece(buf, lane, p);
+      const uint32_t r[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { v[8 * p + 2 * j] += __uint_as_float(r[j] << 16); v[8 * p + 2 * j + 1] += __uint_as_float(r[j] & 0xffff0000u); }
+    }
+  } else {
+    if (lane == 0) tma_store_wait_read<1>();       // the store before the last, from this buffer, has been read
+    __syncwarp();
+  }
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    uint32_t h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * p + 2 * j], v[8 * p + 2 * j + 1]);
+      h[j] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    *staged_piece(buf, lane, p) = make_uint4(h[0], h[1], h[2], h[3]);
+  }
+  fence_proxy_async();
+  __syncwarp();
+  if (lane == 0) {
+    if (row0 < sh.M && left > 0) tma_store_2d(map_out, buf, col, row0);
+    tma_store_commit();
+  }
+  ++w.n;
+  return true;
 }
 
 // ---------------------------------------------------------------------------------------- bias gradient
@@ -218,11 +287,13 @@ __device__ __forceinline__ void bias_gradient_part(const LinEpilogue& e, int row
 template <int KIND, bool SPLIT>
 __global__ void __launch_bounds__(kLtPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_res,
                    const __grid_constant__ LtShape sh, const __grid_constant__ LinEpilogue epi, int split, unsigned* status) {
   constexpr bool a_mn = Layout<KIND>::a_mn, b_mn = Layout<KIND>::b_mn;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  LtBars* bars = reinterpret_cast<LtBars*>(smem + kLtPairStages * 4 * kLtBox);
+  uint8_t* staging = smem + kLtPairStages * 4 * kLtBox;
+  LtBars* bars = reinterpret_cast<LtBars*>(staging + 8 * kLtStaging);
   volatile int* abort_flag = &bars->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t cta = cluster_ctarank(), rank = cta & 1, leader = cta & ~1u;      // rank: which half of the pair
@@ -239,6 +310,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     for (int s = 0; s < kLtPairStages; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(&bars->acc_full[a], 1); mbar_init(&bars->acc_empty[a], 16); }
     mbar_init(&bars->drain, 1);
+    for (int w = 0; w < 8; ++w) mbar_init(&bars->res[w], 1);
     bars->abort_flag = 0;
     bars->never_flag = 0;
     fence_barrier_init();
@@ -257,6 +329,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   if (!SPLIT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   const int q = warp & 3, part = (warp - 2) >> 2;      // epilogue warps: quarter of the lanes; every second 32 columns
+  WayOut way{staging + (warp - 2) * kLtStaging, &bars->res[(warp - 2) & 7], 0u};
+  const bool fetch = KIND == kEpiForward && epi.res && sh.staged;
   bool dead = false;
   if (warp == 0) {
     if (lane == 0) {
@@ -334,31 +408,32 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     uint32_t t = 0;
     if (KIND == kEpiWeight && epi.db) {
       if (!SPLIT) {
-        bias_gradient<8>(epi, sh.M, bars->red);
+        bias_gradient<8>(epi, sh.M, reinterpret_cast<float(*)[128]>(staging));
       } else {
         const int tm = sh.m_fastest ? pair % sh.tiles_m : pair / sh.tiles_n, tn = sh.m_fastest ? pair / sh.tiles_m : pair % sh.tiles_n;
         const int g = bias_share(sh.tiles_n);
         const int64_t t0 = (int64_t)k_begin * kLtK, t1 = (int64_t)k_end * kLtK;
         if (tn * g < 16)
-          bias_gradient_part(epi, sh.M, tm * 256 + (int)rank * 128 + tn * g * 8, g, t0, t1 < epi.tokens ? t1 : epi.tokens, bars->red,
-                             bars->db_part);
+          bias_gradient_part(epi, sh.M, tm * 256 + (int)rank * 128 + tn * g * 8, g, t0, t1 < epi.tokens ? t1 : epi.tokens,
+                             reinterpret_cast<float(*)[128]>(staging), bars->db_part);
       }
     }
     for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
       const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
       const uint32_t ab = t & 1;
+      const int row0 = tm * 256 + (int)rank * 128 + q * 32, row = row0 + lane;
+      if (fetch && !SPLIT) fetch_residual(way, &map_res, lane, tn * sh.bn + part * 32, row0);      // while the MMAs run
       if (!mbar_wait(&bars->acc_full[ab], (t >> 1) & 1, abort_flag)) { dead = true; break; }
       tc_fence_after();
-      const int row = tm * 256 + (int)rank * 128 + q * 32 + lane;
       const uint32_t d = tmem_base + ab * 256 + ((uint32_t)(q * 32) << 16);
-      if (SPLIT) {         // partial sums to this block's shared memory (the pipeline's, idle by now), column after column
-        float* mine = reinterpret_cast<float*>(smem) + q * 32 + lane;
+      if (SPLIT) {         // partial sums to this block's shared memory (the pipeline's, idle by now), four columns a piece
+        float4* mine = reinterpret_cast<float4*>(smem) + q * 32 + lane;
         for (int c = part * 32; c < sh.bn; c += 64) {
           float v[32];
           tmem_ld32(d + c, v);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) mine[(c + j) * 128] = v[j];
+          for (int j = 0; j < 32; j += 4) mine[(c + j) / 4 * 128] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         }
       } else {
         for (int c = part * 32; c < sh.bn; c += 64) {
@@ -369,10 +444,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           __syncwarp();
           tmem_ld32(d + c, v);
           tmem_ld_wait();
-          if (live) epilogue_row32<KIND>(epi, sh, aux, v, row, col);
+          if (live) epilogue_value32<KIND>(epi, sh, aux, v, row, col);
           __syncwarp();
+          if (!way_out<KIND>(way, epi, sh, &map_out, v, row0, lane, col, abort_flag)) { dead = true; break; }
+          if (fetch && c + 64 < sh.bn) fetch_residual(way, &map_res, lane, col + 64, row0);
         }
       }
+      if (dead) break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&bars->acc_empty[ab]), leader));   // the leader's barrier
@@ -397,30 +475,41 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           epi.db[col] = v;
         }
       }
-      const int row = tm * 256 + (int)rank * 128 + q * 32 + lane, blocks = sh.bn / 32;
+      const int row0 = tm * 256 + (int)rank * 128 + q * 32, row = row0 + lane, blocks = sh.bn / 32;
       const int last = blocks * (part_k + 1) / split;
-      for (int blk = blocks * part_k / split + part; blk < last; blk += 2) {
+      for (int blk = blocks * part_k / split + part; blk < last && !dead; blk += 2) {
         const int col = tn * sh.bn + blk * 32;
-        if (row < sh.M && col < sh.N) {
-          float v[32], aux[32];
-          epilogue_aux32<KIND>(epi, sh, aux, row, col);
-          const uint32_t at = smem_u32(smem) + (uint32_t)(blk * 32 * 128 + q * 32 + lane) * 4;
+        const bool live = row < sh.M && col < sh.N;
+        float v[32], aux[32];
+        if (fetch) fetch_residual(way, &map_res, lane, col, row0);
+        if (live) epilogue_aux32<KIND>(epi, sh, aux, row, col);
+        const uint32_t at = smem_u32(smem) + (uint32_t)(blk * 8 * 128 + q * 32 + lane) * 16;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0.f;
-          for (int s = 0; s < split; ++s) {
-            const uint32_t from = map_to_rank(at, 2 * s + rank);
-            float w[32];
+        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+        for (int s = 0; s < split; ++s) {
+          const uint32_t from = map_to_rank(at, 2 * s + rank);
+          float4 w[8];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) w[j] = ld_shared_cluster(from + j * 512);
+          for (int j = 0; j < 8; ++j) w[j] = ld_shared_cluster4(from + j * 2048);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += w[j];
-          }
-          epilogue_row32<KIND>(epi, sh, aux, v, row, col);
+          for (int j = 0; j < 8; ++j) { v[4 * j] += w[j].x; v[4 * j + 1] += w[j].y; v[4 * j + 2] += w[j].z; v[4 * j + 3] += w[j].w; }
         }
+        if (live) epilogue_value32<KIND>(epi, sh, aux, v, row, col);
+        __syncwarp();
+        if (!way_out<KIND>(way, epi, sh, &map_out, v, row0, lane, col, abort_flag)) dead = true;
+      }
+      if (dead && lane == 0) {
+        if (status) atomicOr(status, kDevTimeout);
+        *abort_flag = 1;
       }
     }
     __syncwarp();
   }
+  if (warp >= 2 && lane == 0) {
+    tma_store_wait_all();          // the buffers go with the block
+    if (dead && fetch) mbar_wait(way.bar, way.n & 1, &bars->never_flag);      // a residual block may still be landing
+  }
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();            // nothing of the other blocks is touched after this
@@ -582,7 +671,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
     __syncwarp();
   }
 
-  if (KIND == kEpiWeight && epi.db && warp >= 2) bias_gradient<4>(epi, sh.M, bars->red);
+  if constexpr (KIND == kEpiWeight) {
+    __shared__ float red[4][128];
+    if (epi.db && warp >= 2) bias_gradient<4>(epi, sh.M, red);
+  }
   const int q = warp & 3;
   const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16);
   const int col = tn * 128 + q * 32 + lane;
@@ -603,7 +695,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
   } else {
     // join: every block lays its partial sums in its own shared memory (the pipeline's, which is idle by now), then
     // sums its share of the tile's rows over the blocks of the cluster in their order
-    float* mine = reinterpret_cast<float*>(smem);
+    float4* mine = reinterpret_cast<float4*>(smem);           // [row of the tile / 4][lane]
     if (warp >= 2) {
       dead = !mbar_wait(&bars->acc_full[0], 0, abort_flag);
       tc_fence_after();
@@ -612,27 +704,24 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
         tmem_ld16(d + c, v);
         tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) mine[(c + j) * 128 + q * 32 + lane] = v[j];
+        for (int j = 0; j < 16; j += 4) mine[(c + j) / 4 * 128 + q * 32 + lane] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
       }
     }
     __syncwarp();
     cluster_sync_all();
     if (warp >= 2 && !dead) {
-      const int share = (sh.bn + split - 1) / split, first = part * share;
+      const int share = (sh.bn / 4 + split - 1) / split * 4, first = part * share;
       const int last = first + share < sh.bn ? first + share : sh.bn;
-      const uint32_t base = smem_u32(mine) + (q * 32 + lane) * 4;
+      const uint32_t base = smem_u32(mine) + (q * 32 + lane) * 16;
       for (int c = first; c < last && row0 + c < sh.M; c += 4) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f}, w[8][4];
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float4 w[8];
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {            // all of them on their way before the first is added
-          const uint32_t from = map_to_rank(base, s < split ? s : 0);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[s][j] = s < split && c + j < last ? ld_shared_cluster(from + (c + j) * 512) : 0.f;
-        }
+        for (int s = 0; s < 8; ++s)              // all of them on their way before the first is added
+          if (s < split) w[s] = ld_shared_cluster4(map_to_rank(base, s) + c / 4 * 2048);
 #pragma unroll
         for (int s = 0; s < 8; ++s)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] += w[s][j];
+          if (s < split) { v[0] += w[s].x; v[1] += w[s].y; v[2] += w[s].z; v[3] += w[s].w; }
         // the rows past this block's share belong to the next block
         epilogue_columns<KIND, 4>(epi, sh, v, row0 + c, row0 + last < sh.M ? row0 + last : sh.M, col, bias, lane);
       }
@@ -667,15 +756,16 @@ EncodeTiledFn encode_fn() {
 }
 
 // outer x inner bf16 matrix -> boxes of 64 (inner) x box_outer, 128-byte swizzle
-bool encode(CUtensorMap* out, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer) {
+bool encode(CUtensorMap* out, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer, int box_inner = 64,
+            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
   cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
   cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  cuuint32_t box[2] = {64, (cuuint32_t)box_outer};
+  cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
   cuuint32_t estr[2] = {1, 1};
   return enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // operand of `rows` x K: k fast -> boxes of `box_rows` rows, otherwise boxes of 64 rows x 64
@@ -684,8 +774,9 @@ bool encode_operand(CUtensorMap* out, const LinOperand& o, int64_t rows, int64_t
 }
 
 constexpr int kMaxDevices = 64;
-constexpr size_t kSplitSmemMax = 227 * 1024;
-size_t pair_smem() { return (size_t)kLtPairStages * 4 * kLtBox + sizeof(LtBars) + 1024; }
+constexpr size_t kSplitSmemMax = 224 * 1024;          // 220 KB of stages and the barriers
+constexpr size_t kPairSmem = (size_t)kLtPairStages * 4 * kLtBox + 8 * kLtStaging + sizeof(LtBars) + 1024;
+static_assert(kPairSmem <= 227 * 1024, "shared memory of the pair kernel");
 
 struct Device {
   int n_sm = 0;
@@ -719,7 +810,7 @@ const Device* device() {
   if (d.ready) return &d;
   Device n;
   if (cudaDeviceGetAttribute(&n.n_sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n.n_sm < 2) return nullptr;
-  const int pair = (int)pair_smem(), split = (int)kSplitSmemMax;
+  const int pair = (int)kPairSmem, split = (int)kSplitSmemMax;
   const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
   if (cudaFuncSetAttribute(linear_pair_kernel<kEpiForward, false>, at, pair) != cudaSuccess ||
       cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, false>, at, pair) != cudaSuccess ||
@@ -733,7 +824,7 @@ const Device* device() {
     return nullptr;
   for (int k = 1; k <= 4; ++k) {
     cudaLaunchAttribute attr{};
-    const cudaLaunchConfig_t cfg = config(2u * k, kLtPairThreads, pair_smem(), 2u * k, &attr, nullptr);
+    const cudaLaunchConfig_t cfg = config(2u * k, kLtPairThreads, kPairSmem, 2u * k, &attr, nullptr);
     if (cudaOccupancyMaxActiveClusters(&n.clusters[k], linear_pair_kernel<kEpiForward, true>, &cfg) != cudaSuccess) return nullptr;
     if (n.clusters[k] < 1) n.clusters[k] = 1;
   }
@@ -806,6 +897,12 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
     if (tiles > 0x0fffffff) return SC_ERR_TOO_LARGE;
     sh.m_fastest = p.M <= p.N;
     if (!encode_operand(&a, p.A, p.M, p.K, 128) || !encode_operand(&b, p.B, p.N, p.K, c.bn / 2)) return SC_ERR_CUDA;
+    CUtensorMap o = a, r = a;          // placeholders where the epilogue does not go through shared memory
+    sh.staged = sh.vec && !p.epi.out_f32;
+    if (sh.staged) {
+      if (!encode(&o, p.epi.out, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return SC_ERR_CUDA;
+      if (p.epi.res && !encode(&r, p.epi.res, p.N, p.M, p.epi.ldr, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return SC_ERR_CUDA;
+    }
     const int slots = dev->n_sm / 2;
     const auto go = [&](int64_t begin, int64_t end, int split, bool rest) {
       sh.tile_begin = (int)begin;
@@ -813,15 +910,15 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
       const int64_t pairs = split > 1 ? (end - begin) * split : end - begin < slots ? end - begin : slots;
       LinEpilogue epi = p.epi;
       if (rest) epi.db = nullptr;
-      cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, pair_smem(), 2u * split, attr, s);
+      cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, kPairSmem, 2u * split, attr, s);
       if (rest) {
         attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.numAttrs = 2;
       }
       ++g_kernel_launches;
-      return split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, sh, epi, split, status)
-                       : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, sh, epi, 1, status);
+      return split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, o, r, sh, epi, split, status)
+                       : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, o, r, sh, epi, 1, status);
     };
     // The last wave of a launch that needs more than one is seldom full. It becomes a launch of its own with the contraction
     // split over two to four pairs a tile, which starts on the SMs the full waves leave, where the rounds that takes are
