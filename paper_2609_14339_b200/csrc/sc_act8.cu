@@ -69,6 +69,8 @@ __global__ void __launch_bounds__(256)
 a8_compress_kernel(const void* __restrict__ X, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int blocks,
                    int64_t tokens, int features, int64_t ldx) {
   const A8Place p(tokens, blocks);
+  chain_wait();
+  chain_go();
   if (!p.live) return;
   const int64_t at = p.token * ldx + p.col;
   Eight<F32, VEC> x[kA8Unroll];
@@ -99,6 +101,8 @@ __global__ void __launch_bounds__(256)
 a8_expand_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ qe, int blocks, const void* dA, void* Y,
                  int64_t tokens, int features, int64_t ldda, int64_t ldy) {
   const A8Place p(tokens, blocks);
+  chain_wait();
+  chain_go();
   if (!p.live || p.col >= features) return;
   const int64_t from = p.token * ldda + p.col, to = p.token * ldy + p.col;
   const int n = features - p.col;
@@ -155,9 +159,9 @@ void expand_one(const Act8View& v, const void* dA, void* Y, int64_t tokens, int6
   const int dtype = F32 ? SC_DTYPE_FP32 : SC_DTYPE_BF16, blocks = (int)(v.wide / 32);
   const unsigned grid = grid_for(tokens, v.wide);
   if (vec_ok(Y, ldy, features, dtype) && (!GRAD || vec_ok(dA, ldda, features, dtype)))
-    a8_expand_kernel<F32, ACT, GRAD, true><<<grid, 256, 0, s>>>(v.q, v.e, blocks, dA, Y, tokens, (int)features, ldda, ldy);
+    launch_chained(a8_expand_kernel<F32, ACT, GRAD, true>, dim3(grid), 256, 0, s, v.q, v.e, blocks, dA, Y, tokens, (int)features, ldda, ldy);
   else
-    a8_expand_kernel<F32, ACT, GRAD, false><<<grid, 256, 0, s>>>(v.q, v.e, blocks, dA, Y, tokens, (int)features, ldda, ldy);
+    launch_chained(a8_expand_kernel<F32, ACT, GRAD, false>, dim3(grid), 256, 0, s, v.q, v.e, blocks, dA, Y, tokens, (int)features, ldda, ldy);
 }
 template <bool F32, bool GRAD>
 void expand_act(const Act8View& v, int act, const void* dA, void* Y, int64_t tokens, int64_t features, int64_t ldda,
@@ -196,11 +200,11 @@ extern "C" sc_status sc_act8_compress(const void* X_dev, int dtype, void* act8_d
   const int n = (int)features, blocks = (int)(v.wide / 32);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == SC_DTYPE_BF16) {
-    if (vec) a8_compress_kernel<false, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
-    else a8_compress_kernel<false, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
+    if (vec) launch_chained(a8_compress_kernel<false, true>, dim3(grid), 256, 0, s, X_dev, v.q, v.e, blocks, tokens, n, ldx);
+    else launch_chained(a8_compress_kernel<false, false>, dim3(grid), 256, 0, s, X_dev, v.q, v.e, blocks, tokens, n, ldx);
   } else {
-    if (vec) a8_compress_kernel<true, true><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
-    else a8_compress_kernel<true, false><<<grid, 256, 0, s>>>(X_dev, v.q, v.e, blocks, tokens, n, ldx);
+    if (vec) launch_chained(a8_compress_kernel<true, true>, dim3(grid), 256, 0, s, X_dev, v.q, v.e, blocks, tokens, n, ldx);
+    else launch_chained(a8_compress_kernel<true, false>, dim3(grid), 256, 0, s, X_dev, v.q, v.e, blocks, tokens, n, ldx);
   }
   ++g_kernel_launches;
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;

@@ -181,6 +181,34 @@ struct sc_plan {
 
 namespace sc {
 
+// ---- chained launches ---------------------------------------------------------------------------------------
+// The kernels around the step are short and follow one another on a stream, so each may be set up while the one before it
+// still runs (programmatic dependent launch): every thread calls chain_wait() before it touches global memory, which
+// returns when everything queued before is finished and visible, then chain_go(), after which the next kernel may start
+// its own way to that point.
+#ifdef __CUDACC__
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chain_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+inline void chain_attribute(cudaLaunchAttribute* a) {
+  a->id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  a->val.programmaticStreamSerializationAllowed = 1;
+}
+template <typename... P, typename... A>
+inline void launch_chained(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  chain_attribute(&attr);
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);        // an error stays for cudaGetLastError
+}
+#endif
+
 // ---- host helpers (sc_plan.cu) -------------------------------------------------------------------------
 extern std::atomic<long long> g_kernel_launches;   // kernels this library has launched in this process (all plans)
 sc_status upload_table(sc_plan* p);

@@ -153,6 +153,8 @@ linear_simt_kernel(const __grid_constant__ LinProblem p, unsigned split) {
   SimtLoader<T, A_KFAST, kSimtM> la(p.A, p.M, p.K, m0, first * kSimtK);
   SimtLoader<T, B_KFAST, kSimtN> lb(p.B, p.N, p.K, n0, first * kSimtK);
   float acc[8][8] = {};
+  chain_wait();
+  chain_go();
   if (first < last) {
     la.load(first * kSimtK);
     lb.load(first * kSimtK);
@@ -240,12 +242,13 @@ sc_status simt_kind(const LinProblem& p, cudaStream_t s) {
   cfg.gridDim = dim3((unsigned)(tiles * split));
   cfg.blockDim = dim3(kSimtThreads);
   cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = (unsigned)split;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)split;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  chain_attribute(&attr[1]);
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
   if (cudaLaunchKernelEx(&cfg, linear_simt_kernel<KIND, T, KIND != kEpiWeight, KIND == kEpiForward>, p, (unsigned)split) != cudaSuccess)
     return SC_ERR_CUDA;
   ++g_kernel_launches;
@@ -257,6 +260,8 @@ constexpr int kColSlices = 64;
 template <typename T>
 __global__ void __launch_bounds__(128)
 column_sum_kernel(const T* __restrict__ dY, float* __restrict__ part, int64_t tokens, int64_t rows, int64_t ld) {
+  chain_wait();
+  chain_go();
   const int64_t c = (int64_t)blockIdx.x * 128 + threadIdx.x;
   if (c >= rows) return;
   float s = 0.f;
@@ -265,6 +270,8 @@ column_sum_kernel(const T* __restrict__ dY, float* __restrict__ part, int64_t to
 }
 __global__ void __launch_bounds__(128)
 column_join_kernel(const float* __restrict__ part, float* __restrict__ out, int slices, int64_t rows) {
+  chain_wait();
+  chain_go();
   const int64_t c = (int64_t)blockIdx.x * 128 + threadIdx.x;
   if (c >= rows) return;
   float s = 0.f;
@@ -416,10 +423,10 @@ extern "C" sc_status sc_linear_weight_grad(const void* dY_dev, int operand_dtype
     const int slices = tokens < kColSlices ? (int)tokens : kColSlices;
     const unsigned blocks = (unsigned)((rows + 127) / 128);
     if (operand_dtype == SC_DTYPE_FP32)
-      column_sum_kernel<float><<<dim3(blocks, slices), 128, 0, s>>>(static_cast<const float*>(dY_dev), part, tokens, rows, lddy);
+      launch_chained(column_sum_kernel<float>, dim3(blocks, slices), 128, 0, s, static_cast<const float*>(dY_dev), part, tokens, rows, lddy);
     else
-      column_sum_kernel<bf16><<<dim3(blocks, slices), 128, 0, s>>>(static_cast<const bf16*>(dY_dev), part, tokens, rows, lddy);
-    column_join_kernel<<<blocks, 128, 0, s>>>(part, static_cast<float*>(dbias_dev), slices, rows);
+      launch_chained(column_sum_kernel<bf16>, dim3(blocks, slices), 128, 0, s, static_cast<const bf16*>(dY_dev), part, tokens, rows, lddy);
+    launch_chained(column_join_kernel, dim3(blocks), 128, 0, s, part, static_cast<float*>(dbias_dev), slices, rows);
     g_kernel_launches += 2;
   }
   return linear_run(kEpiWeight, operand_dtype == SC_DTYPE_FP32, p, static_cast<unsigned*>(status_dev), s);

@@ -288,7 +288,8 @@ template <int KIND, bool SPLIT>
 __global__ void __launch_bounds__(kLtPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_res,
-                   const __grid_constant__ LtShape sh, const __grid_constant__ LinEpilogue epi, int split, unsigned* status) {
+                   const __grid_constant__ LtShape sh, const __grid_constant__ LinEpilogue epi, int split, int rest,
+                   unsigned* status) {
   constexpr bool a_mn = Layout<KIND>::a_mn, b_mn = Layout<KIND>::b_mn;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -325,8 +326,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   cluster_sync_all();            // the peer's barriers exist before anything is sent to them
   tc_fence_after();
   const uint32_t tmem_base = bars->tmem_slot;
-  // the launch of the remaining tiles, if there is one, may take the SMs that this one leaves (see launch())
-  if (!SPLIT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // a launch of remaining tiles (see launch()) does not wait for the full waves before it, which have waited for it
+  if (!rest) chain_wait();
+  chain_go();
 
   const int q = warp & 3, part = (warp - 2) >> 2;      // epilogue warps: quarter of the lanes; every second 32 columns
   WayOut way{staging + (warp - 2) * kLtStaging, &bars->res[(warp - 2) & 7], 0u};
@@ -513,36 +515,37 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();            // nothing of the other blocks is touched after this
-  // a launch of remaining tiles runs beside the one before it, but must not be over before that one is
-  if (SPLIT) asm volatile("griddepcontrol.wait;" ::: "memory");
+  // it runs beside them, but must not be over before they are
+  if (rest) chain_wait();
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
 }
 
 // ---------------------------------------------------------------------------------------- split contraction
-// One column of D (a lane of the accumulator) per thread, `count` rows of D at a time.
+// One column of D (a lane of the accumulator) per thread, CNT rows of D at a time, up to rows_end.
+// What comes from global memory: residual, or slopes of the checkpoint. Asked for before the sums are waited for.
 template <int KIND, int CNT>
-__device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtShape& sh, float* v, int64_t row0, int64_t rows_end,
-                                                 int col, float bias, int lane) {
+__device__ __forceinline__ void columns_aux(const LinEpilogue& e, const LtShape& sh, float* aux, int64_t row0, int64_t rows_end, int col) {
   const bool inside = col < sh.N;
-  const int64_t tokens = sh.M;
-  float aux[CNT];
   if (KIND == kEpiForward && e.res) {
 #pragma unroll
     for (int j = 0; j < CNT; ++j) {
       const int64_t i = (row0 + j) * e.ldr + col;
       aux[j] = !(inside && row0 + j < rows_end) ? 0.f
-               : e.out_f32                  ? static_cast<const float*>(e.res)[i]
-                                            : __bfloat162float(static_cast<const bf16*>(e.res)[i]);
+               : e.out_f32                      ? static_cast<const float*>(e.res)[i]
+                                                : __bfloat162float(static_cast<const bf16*>(e.res)[i]);
     }
   } else if (KIND == kEpiInput && e.q) {
 #pragma unroll
-    for (int j = 0; j < CNT; ++j) {
-      const bool ok = inside && row0 + j < rows_end;
-      aux[j] = ok ? (float)e.q[a8_at(tokens, row0 + j, col)] * a8_step(e.e[a8_scale_at(tokens, row0 + j, col)]) : 0.f;
-    }
+    for (int j = 0; j < CNT; ++j)
+      aux[j] = inside && row0 + j < rows_end ? (float)e.q[a8_at(sh.M, row0 + j, col)] * a8_step(e.e[a8_scale_at(sh.M, row0 + j, col)]) : 0.f;
     act_slopes<CNT>(e.act, aux);
   }
+}
+template <int KIND, int CNT>
+__device__ __forceinline__ void columns_out(const LinEpilogue& e, const LtShape& sh, float* v, const float* aux, int64_t row0,
+                                            int64_t rows_end, int col, float bias, int lane) {
+  const bool inside = col < sh.N;
   if (KIND == kEpiForward) {
 #pragma unroll
     for (int j = 0; j < CNT; ++j) v[j] = inside ? v[j] + bias : 0.f;
@@ -552,8 +555,8 @@ __device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtS
         const uint32_t eb = a8_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[j]) & 0x7fffffffu));
         const float inv = a8_inverse(eb);
         if (row0 + j < rows_end && col < e.wide) {
-          e.q[a8_at(tokens, row0 + j, col)] = (int8_t)(inv == 0.f ? 0u : a8_round(v[j], inv) & 255u);
-          if (lane == 0) e.e[a8_scale_at(tokens, row0 + j, col)] = (uint8_t)eb;
+          e.q[a8_at(sh.M, row0 + j, col)] = (int8_t)(inv == 0.f ? 0u : a8_round(v[j], inv) & 255u);
+          if (lane == 0) e.e[a8_scale_at(sh.M, row0 + j, col)] = (uint8_t)eb;
         }
       }
     }
@@ -583,6 +586,10 @@ __device__ __forceinline__ void epilogue_columns(const LinEpilogue& e, const LtS
   }
 }
 
+// Rows of the tile that a block of the cluster finishes, and the room for the other blocks' sums of them.
+__host__ __device__ __forceinline__ int split_share(int bn, int split) { return (bn / 4 + split - 1) / split * 4; }
+__host__ __device__ __forceinline__ uint32_t split_room(int bn, int split) { return split > 1 ? (uint32_t)split_share(bn, split) * split * 512u : 0u; }
+
 // map_l: the operand indexed by D's columns (accumulator lanes), map_r: the one indexed by D's rows.
 template <int KIND>
 __global__ void __launch_bounds__(kLtSplitThreads)
@@ -595,7 +602,8 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
   const int r_boxes = (sh.bn + 63) / 64;
   const uint32_t r_bytes = r_mn ? r_boxes * kLtBox : sh.bn * 128;
   const uint32_t stage_bytes = 2 * kLtBox + r_bytes;
-  LtBars* bars = reinterpret_cast<LtBars*>(smem + (size_t)sh.stages * stage_bytes);
+  uint8_t* room = smem + (size_t)sh.stages * stage_bytes;
+  LtBars* bars = reinterpret_cast<LtBars*>(room + split_room(sh.bn, split));
   volatile int* abort_flag = &bars->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int part = (int)(blockIdx.x % split), tile = (int)(blockIdx.x / split);
@@ -615,6 +623,9 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
   if (warp == 1) tmem_alloc(&bars->tmem_slot, cols_tmem);
   tc_fence_before();
   __syncthreads();
+  if (split > 1) cluster_arrive();         // waited for before anything is sent to a peer: by then it is running
+  chain_wait();
+  chain_go();
   tc_fence_after();
   const uint32_t tmem_base = bars->tmem_slot;
 
@@ -682,52 +693,69 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
   const int64_t row0 = (int64_t)tm * sh.bn;
   if (split == 1) {
     if (warp >= 2) {
-      dead = !mbar_wait(&bars->acc_full[0], 0, abort_flag);
-      tc_fence_after();
       for (int c = 0; c < sh.bn && !dead && row0 + c < sh.M; c += 16) {
-        float v[16];
+        float v[16], aux[16];
+        columns_aux<KIND, 16>(epi, sh, aux, row0 + c, sh.M, col);
+        __syncwarp();
+        if (c == 0 && !mbar_wait(&bars->acc_full[0], 0, abort_flag)) { dead = true; break; }
+        tc_fence_after();
         tmem_ld16(d + c, v);
         tmem_ld_wait();
-        epilogue_columns<KIND, 16>(epi, sh, v, row0 + c, sh.M, col, bias, lane);
+        columns_out<KIND, 16>(epi, sh, v, aux, row0 + c, sh.M, col, bias, lane);
         __syncwarp();
       }
     }
   } else {
-    // join: every block lays its partial sums in its own shared memory (the pipeline's, which is idle by now), then
-    // sums its share of the tile's rows over the blocks of the cluster in their order
-    float4* mine = reinterpret_cast<float4*>(smem);           // [row of the tile / 4][lane]
+    // Join: every block sends its partial sums to the blocks that finish those rows (four rows a piece, lane after lane),
+    // which add them up in the blocks' order. Sent, not fetched: the latency of remote reads and a second barrier, before
+    // which no block could leave, were 2 of 12 us for 37 x 2048 x 8192.
+    const int share = split_share(sh.bn, split), first = part * share;
+    const int64_t end = row0 + (first + share < sh.bn ? first + share : sh.bn), rows_end = end < sh.M ? end : sh.M;
+    const float4* sums = reinterpret_cast<const float4*>(room) + q * 32 + lane;
+    float aux[8];
+    __syncwarp();
+    cluster_wait();
     if (warp >= 2) {
+      columns_aux<KIND, 8>(epi, sh, aux, row0 + first, rows_end, col);
+      __syncwarp();
       dead = !mbar_wait(&bars->acc_full[0], 0, abort_flag);
       tc_fence_after();
-      for (int c = 0; c < sh.bn && !dead; c += 16) {
+      const uint32_t to = smem_u32(sums) + (uint32_t)(part * share) / 4 * 2048;
+      int owner = 0, at = 0;                    // row c of the tile is row `at` of block `owner`'s
+      for (int c = 0; c < sh.bn && !dead && row0 + c < sh.M; c += 16) {
         float v[16];
         tmem_ld16(d + c, v);
         tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) mine[(c + j) / 4 * 128 + q * 32 + lane] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        for (int j = 0; j < 16; j += 4) {
+          st_shared_cluster4(map_to_rank(to, owner) + at / 4 * 2048, v[j], v[j + 1], v[j + 2], v[j + 3]);
+          at += 4;
+          if (at == share) { at = 0; ++owner; }
+        }
       }
     }
     __syncwarp();
     cluster_sync_all();
     if (warp >= 2 && !dead) {
-      const int share = (sh.bn / 4 + split - 1) / split * 4, first = part * share;
-      const int last = first + share < sh.bn ? first + share : sh.bn;
-      const uint32_t base = smem_u32(mine) + (q * 32 + lane) * 16;
-      for (int c = first; c < last && row0 + c < sh.M; c += 4) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        float4 w[8];
+      for (int c = 0; c < share && row0 + first + c < rows_end; c += 8) {
+        if (c > 0) columns_aux<KIND, 8>(epi, sh, aux, row0 + first + c, rows_end, col);
+        float v[8] = {};
 #pragma unroll
-        for (int s = 0; s < 8; ++s)              // all of them on their way before the first is added
-          if (s < split) w[s] = ld_shared_cluster4(map_to_rank(base, s) + c / 4 * 2048);
+        for (int h = 0; h < 2; ++h) {
+          if (c + 4 * h < share) {
 #pragma unroll
-        for (int s = 0; s < 8; ++s)
-          if (s < split) { v[0] += w[s].x; v[1] += w[s].y; v[2] += w[s].z; v[3] += w[s].w; }
-        // the rows past this block's share belong to the next block
-        epilogue_columns<KIND, 4>(epi, sh, v, row0 + c, row0 + last < sh.M ? row0 + last : sh.M, col, bias, lane);
+            for (int s = 0; s < 8; ++s) {
+              if (s < split) {
+                const float4 w = sums[(s * share + c + 4 * h) / 4 * 128];
+                v[4 * h] += w.x; v[4 * h + 1] += w.y; v[4 * h + 2] += w.z; v[4 * h + 3] += w.w;
+              }
+            }
+          }
+        }
+        columns_out<KIND, 8>(epi, sh, v, aux, row0 + first + c, rows_end, col, bias, lane);
+        __syncwarp();
       }
     }
-    __syncwarp();
-    cluster_sync_all();            // the peers have read this block's sums
   }
   if (dead && lane == 0 && warp >= 2) {
     if (status) atomicOr(status, kDevTimeout);
@@ -790,11 +818,12 @@ cudaLaunchConfig_t config(unsigned blocks, int threads, size_t smem, unsigned cl
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  attr->id = cudaLaunchAttributeClusterDimension;
-  attr->val.clusterDim.x = cluster;
-  attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  chain_attribute(&attr[1]);
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   return cfg;
 }
 
@@ -823,8 +852,9 @@ const Device* device() {
       cudaFuncSetAttribute(linear_split_kernel<kEpiWeight>, at, split) != cudaSuccess)
     return nullptr;
   for (int k = 1; k <= 4; ++k) {
-    cudaLaunchAttribute attr{};
-    const cudaLaunchConfig_t cfg = config(2u * k, kLtPairThreads, kPairSmem, 2u * k, &attr, nullptr);
+    cudaLaunchAttribute attr[2] = {};
+    cudaLaunchConfig_t cfg = config(2u * k, kLtPairThreads, kPairSmem, 2u * k, attr, nullptr);
+    cfg.numAttrs = 1;
     if (cudaOccupancyMaxActiveClusters(&n.clusters[k], linear_pair_kernel<kEpiForward, true>, &cfg) != cudaSuccess) return nullptr;
     if (n.clusters[k] < 1) n.clusters[k] = 1;
   }
@@ -844,7 +874,11 @@ struct Choice {
 Choice choose(int kind, int64_t M, int64_t N, int64_t K, const Device& d) {
   const int64_t chunks = up(K, kLtK);
   Choice best;
-  if (M > 128) {
+  const int64_t lane_tiles = up(N, 128);
+  // Up to 128 rows the split kernel, unless they are more than 64 and its tiles fill the chip anyway: the pair kernel's
+  // epilogue then wins (128 x 14336 x 4096: 31 against 33 us, with a residual 34 against 54; 80 x 4096 x 4096 the other way
+  // round: 19 against 15).
+  if (M > 128 || (M > 64 && 4 * lane_tiles >= 3 * d.n_sm)) {
     for (int bn = 256; bn >= 128; bn -= 32) {
       const int64_t tiles = up(M, 256) * up(N, bn);
       const double stage = 500.0 + bn;
@@ -860,16 +894,14 @@ Choice choose(int kind, int64_t M, int64_t N, int64_t K, const Device& d) {
   const int step = kind == kEpiWeight ? 64 : 16;
   const int bn = (int)up(M, step) * step;
   const size_t stage_bytes = 2 * kLtBox + (size_t)bn * 128;
-  // Enough blocks for every SM, two or three of them side by side: one's loads cover another's join. A tile of more than 64
-  // rows that can have three quarters of the SMs without a split is better off without (128 x 14336 x 4096: 36 us, split
-  // in two 41 us); fewer than 33 rows leave room for three blocks per SM (1 x 14336 x 4096: 24.2 us, two blocks 25.2).
-  const int64_t tiles = up(N, 128);
+  // Enough blocks for every SM, two of them side by side (1 x 14336 x 4096: 224 of four stages 24.2 us, 112 of six 28.5): one's
+  // loads cover another's join. More than 64 rows leave room for one, with clusters of up to four: of eight the chip takes
+  // few at a time.
   int split = 1;
-  if (bn <= 64 || 4 * tiles < 3 * d.n_sm)
-    while (split < 8 && tiles * split < d.n_sm && 2 * split <= chunks) split *= 2;
-  int stages = (int)((bn <= 32 ? 74 : bn > 64 && split == 1 ? 220 : 110) * 1024 / stage_bytes);
+  while (split < (bn <= 64 ? 8 : 4) && lane_tiles * split < d.n_sm && 2 * split <= chunks) split *= 2;
+  const size_t budget = (size_t)(bn <= 16 ? 84 : bn <= 64 ? 110 : 220) * 1024;
+  int stages = (int)((budget - split_room(bn, split)) / stage_bytes);
   if (stages > kLtMaxStages) stages = kLtMaxStages;
-  while (split > 1 && (size_t)bn * 512 > (size_t)stages * stage_bytes) split /= 2;       // the partial sums' room
   best = {false, bn, split, stages, 0.0};
   return best;
 }
@@ -910,15 +942,10 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
       const int64_t pairs = split > 1 ? (end - begin) * split : end - begin < slots ? end - begin : slots;
       LinEpilogue epi = p.epi;
       if (rest) epi.db = nullptr;
-      cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, kPairSmem, 2u * split, attr, s);
-      if (rest) {
-        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[1].val.programmaticStreamSerializationAllowed = 1;
-        cfg.numAttrs = 2;
-      }
+      const cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, kPairSmem, 2u * split, attr, s);
       ++g_kernel_launches;
-      return split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, o, r, sh, epi, split, status)
-                       : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, o, r, sh, epi, 1, status);
+      return split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, o, r, sh, epi, split, (int)rest, status)
+                       : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, o, r, sh, epi, 1, 0, status);
     };
     // The last wave of a launch that needs more than one is seldom full. It becomes a launch of its own with the contraction
     // split over two to four pairs a tile, which starts on the SMs the full waves leave, where the rounds that takes are
@@ -944,7 +971,7 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
     const int64_t blocks = (int64_t)sh.tiles_m * sh.tiles_n * c.split;
     if (blocks > 0x7fffffff) return SC_ERR_TOO_LARGE;
     if (!encode_operand(&a, p.A, p.M, p.K, c.bn) || !encode_operand(&b, p.B, p.N, p.K, 128)) return SC_ERR_CUDA;
-    const size_t smem = (size_t)c.stages * (2 * kLtBox + (size_t)c.bn * 128) + sizeof(LtBars) + 1024;
+    const size_t smem = (size_t)c.stages * (2 * kLtBox + (size_t)c.bn * 128) + split_room(c.bn, c.split) + sizeof(LtBars) + 1024;
     const cudaLaunchConfig_t cfg = config((unsigned)blocks, kLtSplitThreads, smem, (unsigned)c.split, attr, s);
     if (cudaLaunchKernelEx(&cfg, linear_split_kernel<KIND>, b, a, sh, p.epi, c.split, status) != cudaSuccess) return SC_ERR_CUDA;
     ++g_kernel_launches;

@@ -183,6 +183,8 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
   typedef Piece<F32, EPT, VEC> P;
   typedef Params<EPT, THREADS> W;
   constexpr int ROWS = EPT == 16 ? 1 : 2, WARPS = THREADS / 32;
+  chain_wait();
+  chain_go();
   W* pw = reinterpret_cast<W*>(param_smem);
   W* pb = pw + 1;
   pw->template fill<VEC>(weight, cols, 1.f);
@@ -321,6 +323,8 @@ norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ we
   constexpr bool RES_AHEAD = AHEAD && !F32;
   int turn = 0;
   const float inv_n = 1.f / (float)cols;
+  chain_wait();
+  chain_go();
   pw.template fill<VEC>(weight, cols, 1.f);
   f2 sw[EPT / 2], sb[EPT / 2];
 #pragma unroll
@@ -397,6 +401,8 @@ norm_forward_wide_kernel(const void* X, const float* __restrict__ weight, const 
                          int64_t rows, int cols, int64_t ldx, int64_t ldy) {
   __shared__ float red[2][2][32];
   int turn = 0;
+  chain_wait();
+  chain_go();
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const int64_t x = r * ldx;
     float s = 0.f, none = 0.f;
@@ -434,6 +440,8 @@ norm_backward_wide_kernel(const void* dY, const void* X, const float* __restrict
                           int64_t lddx) {
   __shared__ float red[2][2][32];
   int turn = 0;
+  chain_wait();
+  chain_go();
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const float mean = stats[r], rstd = stats[rows + r];
     float s[2] = {0.f, 0.f};
@@ -458,6 +466,8 @@ template <bool F32>
 __global__ void __launch_bounds__(128)
 norm_columns_kernel(const void* __restrict__ dY, const void* __restrict__ X, const float* __restrict__ stats,
                     float* __restrict__ part, int64_t rows, int cols, int64_t lddy, int64_t ldx) {
+  chain_wait();
+  chain_go();
   const int c = blockIdx.x * 128 + threadIdx.x;
   if (c >= cols) return;
   float sw = 0.f, sb = 0.f;
@@ -475,6 +485,8 @@ __global__ void __launch_bounds__(kJoinCols * kJoinParts)
 norm_columns_join_kernel(const float* __restrict__ part, int slices, float* __restrict__ dweight,
                          float* __restrict__ dbias, int cols) {
   __shared__ float red[2][kJoinParts][kJoinCols + 1];
+  chain_wait();
+  chain_go();
   const int lane = threadIdx.x % kJoinCols, y = threadIdx.x / kJoinCols, c = blockIdx.x * kJoinCols + lane;
   float sw = 0.f, sb = 0.f;
   if (c < cols) {
@@ -546,8 +558,7 @@ void forward_launch(const Forward& f, cudaStream_t s) {
     }
   }
   const int64_t most = (int64_t)kNormSms * blocks_per_sm(THREADS, 1024), groups = EPT == 16 ? f.rows : (f.rows + 1) / 2;
-  norm_forward_kernel<F32, EPT, VEC, THREADS><<<(unsigned)(groups < most ? groups : most), THREADS, smem, s>>>(
-      f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e, f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
+  launch_chained(norm_forward_kernel<F32, EPT, VEC, THREADS>, dim3((unsigned)(groups < most ? groups : most)), THREADS, smem, s, f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e, f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
 }
 struct Backward {
   const void *dY, *X;
@@ -560,8 +571,7 @@ struct Backward {
 };
 template <bool F32, int EPT, bool VEC, int THREADS>
 void backward_launch(const Backward& f, cudaStream_t s) {
-  norm_backward_kernel<F32, EPT, VEC, THREADS><<<(unsigned)f.slices, THREADS, 0, s>>>(
-      f.dY, f.X, f.w, f.stats, f.R, f.dX, f.part, f.rows, (int)f.cols, f.lddy, f.ldx, f.ldr, f.lddx);
+  launch_chained(norm_backward_kernel<F32, EPT, VEC, THREADS>, dim3((unsigned)f.slices), THREADS, 0, s, f.dY, f.X, f.w, f.stats, f.R, f.dX, f.part, f.rows, (int)f.cols, f.lddy, f.ldx, f.ldr, f.lddx);
 }
 
 // one of the built block sizes for the row's width
@@ -620,10 +630,10 @@ sc_status forward(const Forward& f, int dtype, cudaStream_t s) {
   } else {
     const unsigned grid = (unsigned)(f.rows < (1 << 20) ? f.rows : (1 << 20));
     if (dtype == SC_DTYPE_BF16)
-      norm_forward_wide_kernel<false><<<grid, kWideThreads, 0, s>>>(f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e,
+      launch_chained(norm_forward_wide_kernel<false>, dim3(grid), kWideThreads, 0, s, f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e,
                                                                     f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
     else
-      norm_forward_wide_kernel<true><<<grid, kWideThreads, 0, s>>>(f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e,
+      launch_chained(norm_forward_wide_kernel<true>, dim3(grid), kWideThreads, 0, s, f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e,
                                                                    f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
   }
   ++g_kernel_launches;
@@ -645,19 +655,18 @@ sc_status backward(Backward f, int dtype, float* dw, float* db, cudaStream_t s) 
     const unsigned grid = (unsigned)(f.rows < (1 << 20) ? f.rows : (1 << 20));
     const dim3 cgrid((unsigned)((f.cols + 127) / 128), (unsigned)f.slices);
     if (dtype == SC_DTYPE_BF16) {          // the column sums before dX is written: dX may be dY
-      if (sums) norm_columns_kernel<false><<<cgrid, 128, 0, s>>>(f.dY, f.X, f.stats, part, f.rows, (int)f.cols, f.lddy, f.ldx);
-      norm_backward_wide_kernel<false><<<grid, kWideThreads, 0, s>>>(f.dY, f.X, f.w, f.stats, f.R, f.dX, f.rows, (int)f.cols,
+      if (sums) launch_chained(norm_columns_kernel<false>, cgrid, 128, 0, s, f.dY, f.X, f.stats, part, f.rows, (int)f.cols, f.lddy, f.ldx);
+      launch_chained(norm_backward_wide_kernel<false>, dim3(grid), kWideThreads, 0, s, f.dY, f.X, f.w, f.stats, f.R, f.dX, f.rows, (int)f.cols,
                                                                      f.lddy, f.ldx, f.ldr, f.lddx);
     } else {
-      if (sums) norm_columns_kernel<true><<<cgrid, 128, 0, s>>>(f.dY, f.X, f.stats, part, f.rows, (int)f.cols, f.lddy, f.ldx);
-      norm_backward_wide_kernel<true><<<grid, kWideThreads, 0, s>>>(f.dY, f.X, f.w, f.stats, f.R, f.dX, f.rows, (int)f.cols,
+      if (sums) launch_chained(norm_columns_kernel<true>, cgrid, 128, 0, s, f.dY, f.X, f.stats, part, f.rows, (int)f.cols, f.lddy, f.ldx);
+      launch_chained(norm_backward_wide_kernel<true>, dim3(grid), kWideThreads, 0, s, f.dY, f.X, f.w, f.stats, f.R, f.dX, f.rows, (int)f.cols,
                                                                     f.lddy, f.ldx, f.ldr, f.lddx);
     }
     g_kernel_launches += sums ? 2 : 1;
   }
   if (sums) {
-    norm_columns_join_kernel<<<(unsigned)((f.cols + kJoinCols - 1) / kJoinCols), kJoinCols * kJoinParts, 0, s>>>(
-        part, f.rows > 0 ? f.slices : 0, dw, db, (int)f.cols);
+    launch_chained(norm_columns_join_kernel, dim3((unsigned)((f.cols + kJoinCols - 1) / kJoinCols)), kJoinCols * kJoinParts, 0, s, part, f.rows > 0 ? f.slices : 0, dw, db, (int)f.cols);
     ++g_kernel_launches;
   }
   return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
