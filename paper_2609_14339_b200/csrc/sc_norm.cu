@@ -10,6 +10,7 @@ namespace {
 constexpr int kRowMax = 8192;          // 1024 threads x 8 columns
 constexpr int kWideThreads = 256;      // wider rows: re-read per pass instead
 constexpr int kJoinCols = 32, kJoinParts = 32;
+constexpr int kRingDepth = 3;
 
 constexpr int blocks_per_sm(int threads, int threads_per_sm) {
   return threads_per_sm / threads < 1 ? 1 : threads_per_sm / threads < 16 ? threads_per_sm / threads : 16;
@@ -91,22 +92,32 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// A thread's EPT columns of one row, as they lie in memory. VEC: EPT neighbours from thread * EPT on in 16-byte accesses
-// (the number of columns is a multiple of EPT, so a thread's columns are all inside the row or all outside); otherwise
-// every blockDim-th column, one at a time (any stride, alignment and width, still coalesced). Outside the row: zeros.
+// A thread's EPT columns of one row, as they lie in memory. VEC: pieces of 16 bytes, neighbouring threads' pieces beside
+// one another (the number of columns is a multiple of a piece, so a piece is inside the row or outside); otherwise every
+// blockDim-th column, one at a time (any stride, alignment and width, still coalesced). Outside the row: zeros.
 template <bool F32, int EPT, bool VEC>
 struct Piece {
+  static constexpr int kPiece = F32 ? 4 : 8;          // columns in 16 bytes
   static constexpr int kWords = EPT * (F32 ? 4 : 2) / 4;
   uint32_t w[VEC ? kWords : EPT];
-  __device__ static int col(int i) { return VEC ? (int)threadIdx.x * EPT + i : (int)threadIdx.x + i * (int)blockDim.x; }
-  __device__ static bool in(int i, int cols) { return col(VEC ? 0 : i) < cols; }
+  __device__ static int col(int i) {
+    return VEC ? (i / kPiece * (int)blockDim.x + (int)threadIdx.x) * kPiece + i % kPiece : (int)threadIdx.x + i * (int)blockDim.x;
+  }
+  __device__ static bool in(int i, int cols) { return col(VEC ? i / kPiece * kPiece : i) < cols; }
+  // columns of a row that the block's warp `warp` holds
+  __device__ static float columns_of(int warp, int cols) {
+    constexpr int kRun = VEC ? kPiece : 1;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < EPT; i += kRun) c += min(32 * kRun, max(0, cols - i * (int)blockDim.x - warp * 32 * kRun));
+    return (float)c;
+  }
   __device__ void load(const void* p, int64_t at, int cols) {
     if (VEC) {
-      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + (at + col(0)) * (F32 ? 4 : 2));
-      const bool live = in(0, cols);
 #pragma unroll
       for (int k = 0; k < kWords / 4; ++k) {
-        const uint4 u = live ? src[k] : make_uint4(0u, 0u, 0u, 0u);
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + (at + col(k * kPiece)) * (F32 ? 4 : 2));
+        const uint4 u = in(k * kPiece, cols) ? *src : make_uint4(0u, 0u, 0u, 0u);
         w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
       }
     } else {
@@ -124,12 +135,11 @@ template <bool F32, int EPT, bool VEC>
 __device__ __forceinline__ void store_piece(void* p, int64_t at, int cols, const float* v) {
   typedef Piece<F32, EPT, VEC> P;
   if (VEC) {
-    if (P::in(0, cols)) {
-      if (EPT >= 8) {
 #pragma unroll
-        for (int i = 0; i < EPT; i += 8) store8(p, F32, at + P::col(i), true, 8, v + i);
-      } else {
-        *reinterpret_cast<float4*>(static_cast<float*>(p) + at + P::col(0)) = make_float4(v[0], v[1], v[2], v[3]);
+    for (int i = 0; i < EPT; i += P::kPiece) {
+      if (P::in(i, cols)) {
+        if (F32) *reinterpret_cast<float4*>(static_cast<float*>(p) + at + P::col(i)) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        else store8(p, 0, at + P::col(i), true, 8, v + i);
       }
     }
   } else {
@@ -139,33 +149,27 @@ __device__ __forceinline__ void store_piece(void* p, int64_t at, int cols, const
   }
 }
 
-// EPT fp32 parameters of this thread's columns; 0 outside the row
-template <int EPT, bool VEC>
-__device__ __forceinline__ void load_params(const float* p, int cols, float missing, float* v) {
-  typedef Piece<true, EPT, VEC> P;
-  if (p && VEC && P::in(0, cols)) {
-#pragma unroll
-    for (int i = 0; i < EPT; i += 4) {
-      const float4 f = __ldg(reinterpret_cast<const float4*>(p + P::col(i)));
-      v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) v[i] = P::in(i, cols) ? (p ? __ldg(p + P::col(i)) : missing) : 0.f;
-  }
-}
-
 // The parameters of a thread's columns in shared memory, four at a time and lane after lane: read again for every row
 // instead of held in registers, which the rows in flight need.
 template <int EPT, int THREADS>
 struct Params {
   float4 v[EPT / 4][THREADS];
-  template <bool VEC>
+  // P: the rows' Piece. Outside the row: zeros
+  template <typename P, bool VEC>
   __device__ void fill(const float* p, int cols, float missing) {
-    float w[EPT];
-    load_params<EPT, VEC>(p, cols, missing, w);
 #pragma unroll
-    for (int k = 0; k < EPT / 4; ++k) v[k][threadIdx.x] = make_float4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    for (int k = 0; k < EPT / 4; ++k) {
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (VEC) {
+        if (P::in(4 * k, cols)) f = p ? __ldg(reinterpret_cast<const float4*>(p + P::col(4 * k))) : make_float4(missing, missing, missing, missing);
+      } else {
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = P::in(4 * k + i, cols) ? (p ? __ldg(p + P::col(4 * k + i)) : missing) : 0.f;
+        f = make_float4(w[0], w[1], w[2], w[3]);
+      }
+      v[k][threadIdx.x] = f;
+    }
   }
   __device__ float4 get(int k) const { return v[k][threadIdx.x]; }
 };
@@ -187,65 +191,64 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
   chain_go();
   W* pw = reinterpret_cast<W*>(param_smem);
   W* pb = pw + 1;
-  pw->template fill<VEC>(weight, cols, 1.f);
-  pb->template fill<VEC>(bias, cols, 0.f);
+  pw->template fill<P, VEC>(weight, cols, 1.f);
+  pb->template fill<P, VEC>(bias, cols, 0.f);
   int turn = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float n = (float)cols, inv_n = 1.f / n;
   // columns of this thread's warp, and of the warp this lane stands for in the join
-  const auto columns_of = [&](int w) {
-    if (!VEC) {          // EPT runs of 32 columns, THREADS apart
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) c += min(32, max(0, cols - i * THREADS - w * 32));
-      return (float)c;
-    }
-    return (float)min(32 * EPT, max(0, cols - w * 32 * EPT));
-  };
-  const float n_warp = columns_of(warp), inv_n_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
-  const float n_lane = lane < WARPS ? columns_of(lane) : 0.f;
-  P ahead[ROWS];
+  const float n_warp = P::columns_of(warp, cols), inv_n_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
+  const float n_lane = lane < WARPS ? P::columns_of(lane, cols) : 0.f;
+  // Rows on their way, as they lie in memory: two groups of them, since the next can only be asked for when one arrives
+  // (one group, 32 KB per SM: 4.3 TB/s, the latency's share; 16384 x 8192).
+  constexpr int AHEAD = EPT == 16 ? 2 : 1;
+  P ahead[AHEAD][ROWS];
   const int64_t groups = (rows + ROWS - 1) / ROWS;
-  const auto fetch = [&](int64_t g) {
+  const auto fetch = [&](P* p, int64_t g) {
     if (g < groups) {
 #pragma unroll
       for (int h = 0; h < ROWS; ++h) {
-        if (ROWS * g + h < rows) ahead[h].load(X, (ROWS * g + h) * ldx, cols);
-        else ahead[h] = P{};
+        if (ROWS * g + h < rows) p[h].load(X, (ROWS * g + h) * ldx, cols);
+        else p[h] = P{};
       }
     }
   };
-  fetch(blockIdx.x);
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) fetch(ahead[k], blockIdx.x + (int64_t)k * gridDim.x);
   for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
-    f2 x[ROWS][EPT / 2];
+    P x[ROWS];
 #pragma unroll
-    for (int h = 0; h < ROWS; ++h)
+    for (int h = 0; h < ROWS; ++h) {
+      x[h] = ahead[0][h];
 #pragma unroll
-      for (int i = 0; i < EPT / 2; ++i) x[h][i] = ahead[h].pair(i);
-    fetch(g + gridDim.x);
+      for (int k = 0; k + 1 < AHEAD; ++k) ahead[k][h] = ahead[k + 1][h];
+    }
+    fetch(ahead[AHEAD - 1], g + (int64_t)AHEAD * gridDim.x);
     // Mean and squared deviations of each warp's columns, then joined exactly: sum_w M2_w + n_w (mean_w - mean)^2. As
     // accurate as a second pass with the row's mean, with one barrier instead of two.
     float mean[ROWS], m2[ROWS];
 #pragma unroll
     for (int h = 0; h < ROWS; ++h) {
-      f2 s = x[h][0];
+      f2 s = x[h].pair(0);
 #pragma unroll
-      for (int i = 1; i < EPT / 2; ++i) s = f2_add(s, x[h][i]);
+      for (int i = 1; i < EPT / 2; ++i) s = f2_add(s, x[h].pair(i));
       const float2 p = f2_get(s);
       mean[h] = mean_of(warp_sum(p.x + p.y), n_warp, inv_n_warp);
       const f2 minus = f2_make(-mean[h]);
       f2 v = f2_make(0.f);
 #pragma unroll
       for (int i = 0; i < EPT / 2; ++i) {
-        f2 d = f2_add(x[h][i], minus);
+        f2 d = f2_add(x[h].pair(i), minus);
         if (!VEC) {
           const float2 e = f2_get(d);
           d = f2_make(P::in(2 * i, cols) ? e.x : 0.f, P::in(2 * i + 1, cols) ? e.y : 0.f);
+        } else if (!P::in(2 * i, cols)) {
+          d = f2_make(0.f);
         }
         v = f2_fma(d, d, v);
       }
       const float2 e = f2_get(v);
-      m2[h] = warp_sum(VEC && !P::in(0, cols) ? 0.f : e.x + e.y);
+      m2[h] = warp_sum(e.x + e.y);
     }
     if (WARPS > 1) {
       if (lane == 0)
@@ -272,25 +275,29 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
 #pragma unroll
       for (int k = 0; k < EPT / 4; ++k) {
         const float4 w = pw->get(k), b = pb->get(k);
-        const float2 lo = f2_get(f2_fma(f2_add(x[h][2 * k], minus), f2_mul(scale, f2_make(w.x, w.y)), f2_make(b.x, b.y)));
-        const float2 hi = f2_get(f2_fma(f2_add(x[h][2 * k + 1], minus), f2_mul(scale, f2_make(w.z, w.w)), f2_make(b.z, b.w)));
+        const float2 lo = f2_get(f2_fma(f2_add(x[h].pair(2 * k), minus), f2_mul(scale, f2_make(w.x, w.y)), f2_make(b.x, b.y)));
+        const float2 hi = f2_get(f2_fma(f2_add(x[h].pair(2 * k + 1), minus), f2_mul(scale, f2_make(w.z, w.w)), f2_make(b.z, b.w)));
         y[4 * k] = lo.x; y[4 * k + 1] = lo.y; y[4 * k + 2] = hi.x; y[4 * k + 3] = hi.y;
       }
       if (q) {                 // blocks of 32 columns: 32 / EPT neighbouring threads, or the 32 lanes of a warp
         if (VEC) {
-          uint32_t top = 0;
+          constexpr int kRun = P::kPiece;
 #pragma unroll
-          for (int i = 0; i < EPT; ++i) top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);
+          for (int i = 0; i < EPT; i += kRun) {
+            uint32_t top = 0;
 #pragma unroll
-          for (int o = 1; o < 32 / EPT; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const uint32_t e = a8_scale_byte(top);
-          const float inv = a8_inverse(e);
-          const int c = P::col(0);
-          if (c < wide) {
+            for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(y[i + j]) & 0x7fffffffu);
 #pragma unroll
-            for (int i = 0; i < EPT; i += 4)
-              *reinterpret_cast<uint32_t*>(q + a8_at(rows, r, c + i)) = a8_pack4(y[i], y[i + 1], y[i + 2], y[i + 3], inv);
-            if (threadIdx.x % (32 / EPT) == 0) qe[a8_scale_at(rows, r, c)] = (uint8_t)e;
+            for (int o = 1; o < 32 / kRun; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const uint32_t e = a8_scale_byte(top);
+            const float inv = a8_inverse(e);
+            const int c = P::col(i);
+            if (c < wide) {
+#pragma unroll
+              for (int j = 0; j < kRun; j += 4)
+                *reinterpret_cast<uint32_t*>(q + a8_at(rows, r, c + j)) = a8_pack4(y[i + j], y[i + j + 1], y[i + j + 2], y[i + j + 3], inv);
+              if (threadIdx.x % (32 / kRun) == 0) qe[a8_scale_at(rows, r, c)] = (uint8_t)e;
+            }
           }
         } else {
 #pragma unroll
@@ -310,22 +317,52 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
   }
 }
 
+// A thread's own pieces of rows on their way to shared memory (asynchronous copies of 16 bytes, no registers held): what a
+// thread copies only it reads, so no barrier is involved. A copy outside the row is zeros.
+template <int THREADS, int ARRAYS, int DEPTH>
+struct Ring {
+  uint4 slot[DEPTH][ARRAYS][2][THREADS];
+  __device__ void copy(int s, int a, const void* p, int64_t at, int cols) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int c = (k * THREADS + (int)threadIdx.x) * 8;
+      const bool live = c < cols;
+      const char* src = static_cast<const char*>(p) + (at + (live ? c : 0)) * 2;
+      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(&slot[s][a][k][threadIdx.x]);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+    }
+  }
+  __device__ void take(int s, int a, uint32_t* w) const {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint4 u = slot[s][a][k][threadIdx.x];
+      w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
+    }
+  }
+};
+
 // dX of the block's rows, and the block's share of the column sums, kept in registers over all of them.
 template <bool F32, int EPT, bool VEC, int THREADS>
 __global__ void __launch_bounds__(THREADS, blocks_per_sm(THREADS, EPT == 16 ? 512 : 1024))
 norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ weight, const float* __restrict__ stats,
                      const void* R, void* dX, float* __restrict__ part, int64_t rows, int cols, int64_t lddy, int64_t ldx,
                      int64_t ldr, int64_t lddx) {
+  extern __shared__ uint4 ring_smem[];
   __shared__ float red[2][2][32];
   __shared__ Params<EPT, THREADS> pw;
   typedef Piece<F32, EPT, VEC> P;
-  constexpr bool AHEAD = VEC && !(F32 && EPT == 8);      // the next row on its way, as far as the registers go
+  // 16 bf16 columns a thread: two rows on their way through shared memory (one row, 48 KB per SM, in registers: 5.0 TB/s
+  // for 16384 x 8192). Else the next row in registers, as far as they go.
+  constexpr bool RING = !F32 && VEC && EPT == 16;
+  constexpr bool AHEAD = VEC && !(F32 && EPT == 8) && !RING;
   constexpr bool RES_AHEAD = AHEAD && !F32;
+  typedef Ring<THREADS, 3, kRingDepth> Rows;
+  Rows* ring = reinterpret_cast<Rows*>(ring_smem);
   int turn = 0;
   const float inv_n = 1.f / (float)cols;
   chain_wait();
   chain_go();
-  pw.template fill<VEC>(weight, cols, 1.f);
+  pw.template fill<P, VEC>(weight, cols, 1.f);
   f2 sw[EPT / 2], sb[EPT / 2];
 #pragma unroll
   for (int i = 0; i < EPT / 2; ++i) sw[i] = sb[i] = f2_make(0.f);
@@ -338,14 +375,46 @@ norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ we
     n_mean = stats[r];
     n_rstd = stats[rows + r];
   };
+  const auto fetch_ring = [&](int64_t r, int s) {
+    if (r < rows) {
+      ring->copy(s, 0, X, r * ldx, cols);
+      ring->copy(s, 1, dY, r * lddy, cols);
+      if (R) ring->copy(s, 2, R, r * ldr, cols);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int slot = 0;
+  if (RING) {
+#pragma unroll
+    for (int k = 0; k < kRingDepth - 1; ++k) fetch_ring(blockIdx.x + (int64_t)k * gridDim.x, k);
+    n_mean = stats[blockIdx.x];
+    n_rstd = stats[rows + blockIdx.x];
+  }
   if (AHEAD) fetch(blockIdx.x);
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    if (!AHEAD) fetch(r);
-    const P x = nx, dy = ny;
-    const float mean = n_mean, rstd = n_rstd;
-    P res = nr;
-    if (!RES_AHEAD && R) res.load(R, r * ldr, cols);
-    if (AHEAD && r + gridDim.x < rows) fetch(r + gridDim.x);
+    P x, dy, res;
+    float mean, rstd;
+    if (RING) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRingDepth - 2) : "memory");
+      ring->take(slot, 0, x.w);
+      ring->take(slot, 1, dy.w);
+      if (R) ring->take(slot, 2, res.w);
+      // into the slot of the row before, whose pieces this thread has taken
+      fetch_ring(r + (int64_t)(kRingDepth - 1) * gridDim.x, slot == 0 ? kRingDepth - 1 : slot - 1);
+      slot = slot == kRingDepth - 1 ? 0 : slot + 1;
+      mean = n_mean;
+      rstd = n_rstd;
+      if (r + gridDim.x < rows) { n_mean = stats[r + gridDim.x]; n_rstd = stats[rows + r + gridDim.x]; }
+    } else {
+      if (!AHEAD) fetch(r);
+      x = nx;
+      dy = ny;
+      mean = n_mean;
+      rstd = n_rstd;
+      res = nr;
+      if (!RES_AHEAD && R) res.load(R, r * ldr, cols);
+      if (AHEAD && r + gridDim.x < rows) fetch(r + gridDim.x);
+    }
     const f2 minus = f2_make(-mean), scale = f2_make(rstd);
     f2 s0 = f2_make(0.f), s1 = f2_make(0.f);
 #pragma unroll
@@ -545,18 +614,22 @@ struct Forward {
   Act8View a8;
   int64_t rows, cols, ldx, ldy;
 };
+// A kernel's limit of dynamic shared memory, once per device: the call costs as much as a launch.
+template <auto KERNEL>
+void raise_smem(int bytes) {
+  static std::atomic<uint64_t> raised{0};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (!(raised.load(std::memory_order_relaxed) >> (dev & 63) & 1)) {
+    cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    raised.fetch_or(1ull << (dev & 63), std::memory_order_relaxed);
+  }
+}
+
 template <bool F32, int EPT, bool VEC, int THREADS>
 void forward_launch(const Forward& f, cudaStream_t s) {
   const int smem = 2 * (int)sizeof(Params<EPT, THREADS>);
-  if (smem > 40 * 1024) {          // once per device: the call costs as much as a launch
-    static std::atomic<uint64_t> raised{0};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (!(raised.load(std::memory_order_relaxed) >> (dev & 63) & 1)) {
-      cudaFuncSetAttribute(norm_forward_kernel<F32, EPT, VEC, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      raised.fetch_or(1ull << (dev & 63), std::memory_order_relaxed);
-    }
-  }
+  if (smem > 40 * 1024) raise_smem<norm_forward_kernel<F32, EPT, VEC, THREADS>>(smem);
   const int64_t most = (int64_t)kNormSms * blocks_per_sm(THREADS, 1024), groups = EPT == 16 ? f.rows : (f.rows + 1) / 2;
   launch_chained(norm_forward_kernel<F32, EPT, VEC, THREADS>, dim3((unsigned)(groups < most ? groups : most)), THREADS, smem, s, f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e, f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
 }
@@ -571,7 +644,10 @@ struct Backward {
 };
 template <bool F32, int EPT, bool VEC, int THREADS>
 void backward_launch(const Backward& f, cudaStream_t s) {
-  launch_chained(norm_backward_kernel<F32, EPT, VEC, THREADS>, dim3((unsigned)f.slices), THREADS, 0, s, f.dY, f.X, f.w, f.stats, f.R, f.dX, f.part, f.rows, (int)f.cols, f.lddy, f.ldx, f.ldr, f.lddx);
+  const int smem = !F32 && VEC && EPT == 16 ? (int)sizeof(Ring<THREADS, 3, kRingDepth>) : 0;
+  if (smem > 14 * 1024) raise_smem<norm_backward_kernel<F32, EPT, VEC, THREADS>>(smem);
+  launch_chained(norm_backward_kernel<F32, EPT, VEC, THREADS>, dim3((unsigned)f.slices), THREADS, smem, s, f.dY, f.X, f.w,
+                 f.stats, f.R, f.dX, f.part, f.rows, (int)f.cols, f.lddy, f.ldx, f.ldr, f.lddx);
 }
 
 // one of the built block sizes for the row's width
@@ -603,8 +679,8 @@ struct GoBackward {
 template <bool F32>
 void forward_rows(const Forward& f, bool vec, cudaStream_t s) {
   const GoForward go{f};
-  if (!F32 && vec && f.cols % 16 == 0) by_threads<F32, F32 ? 8 : 16, true>(row_threads(f.cols, 16), go, s);
-  else if (vec && f.cols % 8 == 0) by_threads<F32, 8, true>(row_threads(f.cols, 8), go, s);
+  if (!F32 && vec && f.cols % 8 == 0) by_threads<F32, F32 ? 8 : 16, true>(row_threads(f.cols, 16), go, s);
+  else if (F32 && vec && f.cols % 4 == 0) by_threads<true, 8, true>(row_threads(f.cols, 8), go, s);
   else by_threads<F32, 8, false>(row_threads(f.cols, 8), go, s);
 }
 template <bool F32>
@@ -613,10 +689,10 @@ void backward_rows(const Backward& f, bool vec, cudaStream_t s) {
   if (F32 && f.cols <= 4096) {
     if (vec && f.cols % 4 == 0) by_threads<F32, F32 ? 4 : 8, true>(row_threads(f.cols, 4), go, s);
     else by_threads<F32, F32 ? 4 : 8, false>(row_threads(f.cols, 4), go, s);
-  } else if (!F32 && vec && f.cols % 16 == 0) {
+  } else if (!F32 && vec && f.cols % 8 == 0) {
     by_threads<F32, F32 ? 8 : 16, true>(row_threads(f.cols, 16), go, s);
   } else {
-    if (vec && f.cols % 8 == 0) by_threads<F32, 8, true>(row_threads(f.cols, 8), go, s);
+    if (F32 && vec && f.cols % 4 == 0) by_threads<true, 8, true>(row_threads(f.cols, 8), go, s);
     else by_threads<F32, 8, false>(row_threads(f.cols, 8), go, s);
   }
 }

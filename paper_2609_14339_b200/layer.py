@@ -126,6 +126,19 @@ def _weight_grad_bytes(dtype: int, tokens: int, rows: int, cols: int) -> int:
     return int(need)
 
 
+_KEEP = 16 << 20
+_workspaces = {}
+
+
+def _kept_workspace(device: int, queue: int, need: int) -> int:
+    """Workspace of at most _KEEP bytes, kept per stream: what is queued there uses it in turn."""
+    held = _workspaces.get((device, queue))
+    if held is None or held.numel() < need:
+        held = torch.empty((max(need, 1 << 20),), dtype=_U8, device=torch.device("cuda", device))
+        _workspaces[(device, queue)] = held
+    return held.data_ptr()
+
+
 class Act8:
     """An activation kept in 8 bits: blocks of 32 features share a power of two (33 bytes for 32 values)."""
 
@@ -208,12 +221,11 @@ def layer_norm_backward(dY, X, weight, stats, residual_grad=None, out=None, dwei
         dweight = stats.new_empty((cols,))
     if dbias is None:
         dbias = stats.new_empty((cols,))
-    if workspace is None:
-        workspace = X.new_empty((need,), dtype=_U8)
+    queue = _raw_stream(dev)
+    ws = _kept_workspace(dev, queue, need) if workspace is None else _buffer("workspace", workspace, need, dev)
     _done(lib.sc_layernorm_backward(dY.data_ptr(), X.data_ptr(), _DTYPES[dt], w, st, r, out.data_ptr(),
                                     _vector("dweight", dweight, cols, dev), _vector("dbias", dbias, cols, dev), rows,
-                                    cols, lddy, ldx, ldr, lddx, _buffer("workspace", workspace, need, dev),
-                                    workspace.numel(), _raw_stream(dev)), "sc_layernorm_backward")
+                                    cols, lddy, ldx, ldr, lddx, ws, need, queue), "sc_layernorm_backward")
     return out, dweight, dbias
 
 
@@ -340,10 +352,15 @@ def linear_weight_grad(dY, saved, act="none", scale: float = 1.0, out=None, out_
         raise ValueError("out must be contiguous")
     if dbias is None:
         dbias = dY.new_empty((rows,), dtype=_F32)
-    if workspace is None:
+    queue = _raw_stream(dev)
+    if workspace is not None:
+        ws = _buffer("workspace", workspace, need, dev)
+    elif need <= _KEEP:
+        ws = _kept_workspace(dev, queue, need)
+    else:                                   # the size of an activation: goes back to the stream's pool
         workspace = dY.new_empty((need,), dtype=_U8)
+        ws = workspace.data_ptr()
     _done(lib.sc_linear_weight_grad(dY.data_ptr(), _DTYPES[dt], a8, a, scale, out.data_ptr(), _DTYPES[odt],
-                                    _vector("dbias", dbias, rows, dev), tokens, rows, cols, lddy,
-                                    _buffer("workspace", workspace, need, dev), workspace.numel(),
-                                    _status(status, dev), _raw_stream(dev)), "sc_linear_weight_grad")
+                                    _vector("dbias", dbias, rows, dev), tokens, rows, cols, lddy, ws, need,
+                                    _status(status, dev), queue), "sc_linear_weight_grad")
     return out, dbias
