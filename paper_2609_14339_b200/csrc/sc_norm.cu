@@ -154,76 +154,126 @@ __device__ __forceinline__ void store_piece(void* p, int64_t at, int cols, const
 template <int EPT, int THREADS>
 struct Params {
   float4 v[EPT / 4][THREADS];
-  // P: the rows' Piece. Outside the row: zeros
+  // Four of a thread's columns (P: the rows' Piece). Outside the row: zeros
+  template <typename P, bool VEC>
+  __device__ static float4 of(const float* p, int cols, float missing, int k) {
+    if (VEC) {
+      if (!P::in(4 * k, cols)) return make_float4(0.f, 0.f, 0.f, 0.f);
+      return p ? __ldg(reinterpret_cast<const float4*>(p + P::col(4 * k))) : make_float4(missing, missing, missing, missing);
+    }
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = P::in(4 * k + i, cols) ? (p ? __ldg(p + P::col(4 * k + i)) : missing) : 0.f;
+    return make_float4(w[0], w[1], w[2], w[3]);
+  }
   template <typename P, bool VEC>
   __device__ void fill(const float* p, int cols, float missing) {
 #pragma unroll
-    for (int k = 0; k < EPT / 4; ++k) {
-      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (VEC) {
-        if (P::in(4 * k, cols)) f = p ? __ldg(reinterpret_cast<const float4*>(p + P::col(4 * k))) : make_float4(missing, missing, missing, missing);
-      } else {
-        float w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = P::in(4 * k + i, cols) ? (p ? __ldg(p + P::col(4 * k + i)) : missing) : 0.f;
-        f = make_float4(w[0], w[1], w[2], w[3]);
-      }
-      v[k][threadIdx.x] = f;
-    }
+    for (int k = 0; k < EPT / 4; ++k) v[k][threadIdx.x] = of<P, VEC>(p, cols, missing, k);
   }
   __device__ float4 get(int k) const { return v[k][threadIdx.x]; }
 };
 
-// A block takes ROWS neighbouring rows at a time, which share barriers, shuffles and parameters; the next ones are on their
-// way meanwhile. With 8 columns a thread two rows are what makes the shared work small; with 16 one row's is, and a second
-// would not fit the 64 registers that let two blocks of 512 share an SM.
+// A thread's own pieces of rows on their way to shared memory (asynchronous copies of 16 bytes, no registers held): what a
+// thread copies only it reads, so no barrier is involved. A copy outside the row is zeros.
+template <int THREADS, int ARRAYS, int DEPTH>
+struct Ring {
+  uint4 slot[DEPTH][ARRAYS][2][THREADS];
+  __device__ void copy(int s, int a, const void* p, int64_t at, int cols) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int c = (k * THREADS + (int)threadIdx.x) * 8;
+      const bool live = c < cols;
+      const char* src = static_cast<const char*>(p) + (at + (live ? c : 0)) * 2;
+      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(&slot[s][a][k][threadIdx.x]);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+    }
+  }
+  __device__ void take(int s, int a, uint32_t* w) const {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint4 u = slot[s][a][k][threadIdx.x];
+      w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
+    }
+  }
+};
+
+// A block takes two neighbouring rows at a time, which share barriers and parameters; the next ones are on their way
+// meanwhile: with 16 bf16 columns a thread two pairs through shared memory, the parameters in registers (kept in shared
+// memory, beside rows in registers, their reads were a third of that pipe's work: 108 us for 16384 x 8192); else one pair
+// in registers and the parameters in shared memory.
 template <bool F32, int EPT, bool VEC, int THREADS>
-__global__ void __launch_bounds__(THREADS, blocks_per_sm(THREADS, 1024))
+__global__ void __launch_bounds__(THREADS, blocks_per_sm(THREADS, EPT == 16 ? 512 : 1024))
 norm_forward_kernel(const void* X, const float* __restrict__ weight, const float* __restrict__ bias, float eps, void* Y,
                     float* __restrict__ stats, int8_t* __restrict__ q, uint8_t* __restrict__ qe, int64_t wide, int64_t rows,
                     int cols, int64_t ldx, int64_t ldy) {
-  extern __shared__ float4 param_smem[];
+  extern __shared__ float4 forward_smem[];
   __shared__ float2 red[2][2][32];
   typedef Piece<F32, EPT, VEC> P;
   typedef Params<EPT, THREADS> W;
-  constexpr int ROWS = EPT == 16 ? 1 : 2, WARPS = THREADS / 32;
+  constexpr bool RING = EPT == 16;
+  constexpr int ROWS = 2, WARPS = THREADS / 32;
+  typedef Ring<THREADS, ROWS, kRingDepth> Rows;
+  Rows* ring = reinterpret_cast<Rows*>(forward_smem);
   chain_wait();
   chain_go();
-  W* pw = reinterpret_cast<W*>(param_smem);
+  W* pw = reinterpret_cast<W*>(forward_smem);
   W* pb = pw + 1;
-  pw->template fill<P, VEC>(weight, cols, 1.f);
-  pb->template fill<P, VEC>(bias, cols, 0.f);
+  float4 w[RING ? EPT / 4 : 1], b[RING ? EPT / 4 : 1];
+  if (RING) {
+#pragma unroll
+    for (int k = 0; k < EPT / 4; ++k) {
+      w[RING ? k : 0] = W::template of<P, VEC>(weight, cols, 1.f, k);
+      b[RING ? k : 0] = W::template of<P, VEC>(bias, cols, 0.f, k);
+    }
+  } else {
+    pw->template fill<P, VEC>(weight, cols, 1.f);
+    pb->template fill<P, VEC>(bias, cols, 0.f);
+  }
   int turn = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float n = (float)cols, inv_n = 1.f / n;
   // columns of this thread's warp, and of the warp this lane stands for in the join
   const float n_warp = P::columns_of(warp, cols), inv_n_warp = n_warp > 0.f ? 1.f / n_warp : 0.f;
   const float n_lane = lane < WARPS ? P::columns_of(lane, cols) : 0.f;
-  // Rows on their way, as they lie in memory: two groups of them, since the next can only be asked for when one arrives
-  // (one group, 32 KB per SM: 4.3 TB/s, the latency's share; 16384 x 8192).
-  constexpr int AHEAD = EPT == 16 ? 2 : 1;
-  P ahead[AHEAD][ROWS];
+  P ahead[ROWS];
   const int64_t groups = (rows + ROWS - 1) / ROWS;
-  const auto fetch = [&](P* p, int64_t g) {
+  const auto fetch = [&](int64_t g) {
     if (g < groups) {
 #pragma unroll
       for (int h = 0; h < ROWS; ++h) {
-        if (ROWS * g + h < rows) p[h].load(X, (ROWS * g + h) * ldx, cols);
-        else p[h] = P{};
+        if (ROWS * g + h < rows) ahead[h].load(X, (ROWS * g + h) * ldx, cols);
+        else ahead[h] = P{};
       }
     }
   };
+  const auto fetch_ring = [&](int64_t g, int s) {
+    if (g < groups) {
+      ring->copy(s, 0, X, ROWS * g * ldx, cols);
+      if (ROWS * g + 1 < rows) ring->copy(s, 1, X, (ROWS * g + 1) * ldx, cols);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int slot = 0;
+  if (RING) {
 #pragma unroll
-  for (int k = 0; k < AHEAD; ++k) fetch(ahead[k], blockIdx.x + (int64_t)k * gridDim.x);
+    for (int k = 0; k < kRingDepth - 1; ++k) fetch_ring(blockIdx.x + (int64_t)k * gridDim.x, k);
+  } else {
+    fetch(blockIdx.x);
+  }
   for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
     P x[ROWS];
+    if (RING) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRingDepth - 2) : "memory");
 #pragma unroll
-    for (int h = 0; h < ROWS; ++h) {
-      x[h] = ahead[0][h];
+      for (int h = 0; h < ROWS; ++h) ring->take(slot, h, x[h].w);       // a second row past the end: an older one, not stored
+      fetch_ring(g + (int64_t)(kRingDepth - 1) * gridDim.x, slot == 0 ? kRingDepth - 1 : slot - 1);
+      slot = slot == kRingDepth - 1 ? 0 : slot + 1;
+    } else {
 #pragma unroll
-      for (int k = 0; k + 1 < AHEAD; ++k) ahead[k][h] = ahead[k + 1][h];
+      for (int h = 0; h < ROWS; ++h) x[h] = ahead[h];
+      fetch(g + gridDim.x);
     }
-    fetch(ahead[AHEAD - 1], g + (int64_t)AHEAD * gridDim.x);
     // Mean and squared deviations of each warp's columns, then joined exactly: sum_w M2_w + n_w (mean_w - mean)^2. As
     // accurate as a second pass with the row's mean, with one barrier instead of two.
     float mean[ROWS], m2[ROWS];
@@ -274,9 +324,9 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
       float y[EPT];            // outside the row: 0 (weight and bias are 0 there)
 #pragma unroll
       for (int k = 0; k < EPT / 4; ++k) {
-        const float4 w = pw->get(k), b = pb->get(k);
-        const float2 lo = f2_get(f2_fma(f2_add(x[h].pair(2 * k), minus), f2_mul(scale, f2_make(w.x, w.y)), f2_make(b.x, b.y)));
-        const float2 hi = f2_get(f2_fma(f2_add(x[h].pair(2 * k + 1), minus), f2_mul(scale, f2_make(w.z, w.w)), f2_make(b.z, b.w)));
+        const float4 wk = RING ? w[RING ? k : 0] : pw->get(k), bk = RING ? b[RING ? k : 0] : pb->get(k);
+        const float2 lo = f2_get(f2_fma(f2_add(x[h].pair(2 * k), minus), f2_mul(scale, f2_make(wk.x, wk.y)), f2_make(bk.x, bk.y)));
+        const float2 hi = f2_get(f2_fma(f2_add(x[h].pair(2 * k + 1), minus), f2_mul(scale, f2_make(wk.z, wk.w)), f2_make(bk.z, bk.w)));
         y[4 * k] = lo.x; y[4 * k + 1] = lo.y; y[4 * k + 2] = hi.x; y[4 * k + 3] = hi.y;
       }
       if (q) {                 // blocks of 32 columns: 32 / EPT neighbouring threads, or the 32 lanes of a warp
@@ -316,30 +366,6 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
     }
   }
 }
-
-// A thread's own pieces of rows on their way to shared memory (asynchronous copies of 16 bytes, no registers held): what a
-// thread copies only it reads, so no barrier is involved. A copy outside the row is zeros.
-template <int THREADS, int ARRAYS, int DEPTH>
-struct Ring {
-  uint4 slot[DEPTH][ARRAYS][2][THREADS];
-  __device__ void copy(int s, int a, const void* p, int64_t at, int cols) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int c = (k * THREADS + (int)threadIdx.x) * 8;
-      const bool live = c < cols;
-      const char* src = static_cast<const char*>(p) + (at + (live ? c : 0)) * 2;
-      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(&slot[s][a][k][threadIdx.x]);
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-    }
-  }
-  __device__ void take(int s, int a, uint32_t* w) const {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint4 u = slot[s][a][k][threadIdx.x];
-      w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w;
-    }
-  }
-};
 
 // dX of the block's rows, and the block's share of the column sums, kept in registers over all of them.
 template <bool F32, int EPT, bool VEC, int THREADS>
@@ -628,9 +654,9 @@ void raise_smem(int bytes) {
 
 template <bool F32, int EPT, bool VEC, int THREADS>
 void forward_launch(const Forward& f, cudaStream_t s) {
-  const int smem = 2 * (int)sizeof(Params<EPT, THREADS>);
+  const int smem = EPT == 16 ? (int)sizeof(Ring<THREADS, 2, kRingDepth>) : 2 * (int)sizeof(Params<EPT, THREADS>);
   if (smem > 40 * 1024) raise_smem<norm_forward_kernel<F32, EPT, VEC, THREADS>>(smem);
-  const int64_t most = (int64_t)kNormSms * blocks_per_sm(THREADS, 1024), groups = EPT == 16 ? f.rows : (f.rows + 1) / 2;
+  const int64_t most = (int64_t)kNormSms * blocks_per_sm(THREADS, EPT == 16 ? 512 : 1024), groups = (f.rows + 1) / 2;
   launch_chained(norm_forward_kernel<F32, EPT, VEC, THREADS>, dim3((unsigned)(groups < most ? groups : most)), THREADS, smem, s, f.X, f.w, f.b, f.eps, f.Y, f.stats, f.a8.q, f.a8.e, f.a8.wide, f.rows, (int)f.cols, f.ldx, f.ldy);
 }
 struct Backward {
@@ -673,27 +699,28 @@ struct GoBackward {
   void go(cudaStream_t s) const { backward_launch<F32, EPT, VEC, THREADS>(f, s); }
 };
 
-// Columns per thread. The shuffles, barriers and addresses of a row cost the same for 8 columns as for 16, so bf16 rows
-// take 16 where the width allows it (one row's pieces are then 32 bytes a thread); fp32 rows 8, and the backward kernel 4
-// up to 4096 columns (three pieces of a row and the column sums have to fit in registers).
+// Columns per thread. The shuffles, barriers and addresses of a row cost the same for 8 columns as for 16, so bf16 rows of
+// whole 16-byte pieces take 16; fp32 rows 8, and the backward kernel 4 up to 4096 columns (three pieces of a row and the
+// column sums have to fit in registers). Other rows: 8 single columns (fp32 backward 4).
 template <bool F32>
 void forward_rows(const Forward& f, bool vec, cudaStream_t s) {
   const GoForward go{f};
-  if (!F32 && vec && f.cols % 8 == 0) by_threads<F32, F32 ? 8 : 16, true>(row_threads(f.cols, 16), go, s);
-  else if (F32 && vec && f.cols % 4 == 0) by_threads<true, 8, true>(row_threads(f.cols, 8), go, s);
+  constexpr int kEach = F32 ? 8 : 16;
+  if (vec && f.cols % (F32 ? 4 : 8) == 0) by_threads<F32, kEach, true>(row_threads(f.cols, kEach), go, s);
   else by_threads<F32, 8, false>(row_threads(f.cols, 8), go, s);
 }
 template <bool F32>
 void backward_rows(const Backward& f, bool vec, cudaStream_t s) {
   const GoBackward go{f};
-  if (F32 && f.cols <= 4096) {
-    if (vec && f.cols % 4 == 0) by_threads<F32, F32 ? 4 : 8, true>(row_threads(f.cols, 4), go, s);
-    else by_threads<F32, F32 ? 4 : 8, false>(row_threads(f.cols, 4), go, s);
-  } else if (!F32 && vec && f.cols % 8 == 0) {
-    by_threads<F32, F32 ? 8 : 16, true>(row_threads(f.cols, 16), go, s);
+  if constexpr (F32) {
+    const bool pieces = vec && f.cols % 4 == 0, narrow = f.cols <= 4096;
+    if (pieces && narrow) by_threads<true, 4, true>(row_threads(f.cols, 4), go, s);
+    else if (narrow) by_threads<true, 4, false>(row_threads(f.cols, 4), go, s);
+    else if (pieces) by_threads<true, 8, true>(row_threads(f.cols, 8), go, s);
+    else by_threads<true, 8, false>(row_threads(f.cols, 8), go, s);
   } else {
-    if (F32 && vec && f.cols % 4 == 0) by_threads<true, 8, true>(row_threads(f.cols, 8), go, s);
-    else by_threads<F32, 8, false>(row_threads(f.cols, 8), go, s);
+    if (vec && f.cols % 8 == 0) by_threads<false, 16, true>(row_threads(f.cols, 16), go, s);
+    else by_threads<false, 8, false>(row_threads(f.cols, 8), go, s);
   }
 }
 
