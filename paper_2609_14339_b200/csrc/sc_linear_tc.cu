@@ -27,6 +27,14 @@ constexpr int kLtBox = 64 * kLtK * 2;          // one 64 x 64 bf16 box: 8 KB
 constexpr int kLtPairStages = 6;
 constexpr int kLtMaxStages = 8;
 constexpr int kLtStaging = 4096;              // per epilogue warp: two 32 x 32 bf16 blocks
+// The tensor core truncates when it adds to an accumulator: a sum comes out too small by some 1.5e-8 of itself per 16 terms
+// (4.4e-6 after 4096 terms of random sign, 1.4e-5 of one sign). A bf16 result does not show that, an fp32 gradient summed
+// over many tokens does: its accumulators are added up in fp32 after every kLtSegment stages at most (768 terms; 16384
+// tokens: 1.9e-5 off without, 1.4e-7 with). For pairs of SMs that costs time, since reading 128 KB of accumulators beside
+// the MMAs takes about as long as 12 stages (2048 x 8192 x 2048: 58 us without, 68 with), so it is left to fp32 gradients;
+// the forward product does without whatever its result's type, so that the type and a checkpoint change nothing in its
+// sums. With few rows several accumulators fit beside one another and cost nothing.
+constexpr int kLtSegment = 12;
 constexpr int kLtPairThreads = 320;            // producer, issuer, 8 epilogue warps
 constexpr int kLtSplitThreads = 192;           // producer, issuer, 4 epilogue warps
 
@@ -37,7 +45,7 @@ struct LtShape {
   int tiles_m, tiles_n;    // pair: 256-row x bn-column tiles of D; split: bn-row x 128-column tiles of D
   int tile_begin, tile_end;    // pair: the tiles of this launch
   int m_fastest;           // pair: which way consecutive tiles run
-  int stages;              // split
+  int stages, accs;        // split
   int vec;                 // out and res take 16-byte accesses
   int staged;              // pair: bf16 out (and res) that TMA can describe; the epilogue goes through shared memory
   int vec_bias;
@@ -283,8 +291,8 @@ __device__ __forceinline__ void bias_gradient_part(const LinEpilogue& e, int row
 }
 
 // ---------------------------------------------------------------------------------------- two SMs per 256 x bn tile
-// Launched in clusters of 2 * split blocks; blocks 2p and 2p + 1 are pair p of the cluster.
-template <int KIND, bool SPLIT>
+// Launched in clusters of 2 * split blocks; blocks 2p and 2p + 1 are pair p of the cluster. PROMOTE: see kLtSegment.
+template <int KIND, bool SPLIT, bool PROMOTE>
 __global__ void __launch_bounds__(kLtPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_res,
@@ -303,6 +311,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int n_pairs = SPLIT ? (int)(gridDim.x / (2 * split)) : gridDim.x >> 1;
   const int k_begin = SPLIT ? (int)((int64_t)sh.kchunks * part_k / split) : 0;
   const int k_end = SPLIT ? (int)((int64_t)sh.kchunks * (part_k + 1) / split) : sh.kchunks;
+  const int segments = PROMOTE ? (k_end - k_begin + kLtSegment - 1) / kLtSegment : 1;
+  const int seg_len = PROMOTE ? (k_end - k_begin + segments - 1) / segments : k_end - k_begin;
   const int tiles = sh.tile_end, half = sh.bn / 2;
   const int b_boxes = (half + 63) / 64;
   const uint32_t stage_bytes = 2 * kLtBox + (b_mn ? b_boxes * kLtBox : half * 128);     // what TMA writes per block
@@ -377,24 +387,27 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       const uint32_t idesc = umma_idesc_bf16_any(256, sh.bn, a_mn, b_mn);
-      uint32_t it = 0, t = 0;
-      for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
-        const uint32_t ab = t & 1;
-        if (!mbar_wait(&bars->acc_empty[ab], ((t >> 1) & 1) ^ 1, abort_flag)) { dead = true; break; }
-        tc_fence_after();
-        const uint32_t d = tmem_base + ab * 256;
-        for (int kc = k_begin; kc < k_end; ++kc, ++it) {
-          const int s = it % kLtPairStages;
-          if (!mbar_wait(&bars->full[s], (it / kLtPairStages) & 1, abort_flag)) { dead = true; break; }
+      uint32_t it = 0, t = 0;                    // stages, accumulators
+      for (int tile = pair; tile < tiles && !dead; tile += n_pairs) {
+        for (int k0 = k_begin; k0 < k_end && !dead; k0 += seg_len, ++t) {
+          const uint32_t ab = t & 1;
+          if (!mbar_wait(&bars->acc_empty[ab], ((t >> 1) & 1) ^ 1, abort_flag)) { dead = true; break; }
           tc_fence_after();
-          const uint32_t a0 = smem_u32(smem + (size_t)s * 4 * kLtBox), b0 = a0 + 2 * kLtBox;
+          const uint32_t d = tmem_base + ab * 256;
+          const int k1 = k0 + seg_len < k_end ? k0 + seg_len : k_end;
+          for (int kc = k0; kc < k1; ++kc, ++it) {
+            const int s = it % kLtPairStages;
+            if (!mbar_wait(&bars->full[s], (it / kLtPairStages) & 1, abort_flag)) { dead = true; break; }
+            tc_fence_after();
+            const uint32_t a0 = smem_u32(smem + (size_t)s * 4 * kLtBox), b0 = a0 + 2 * kLtBox;
 #pragma unroll
-          for (int k = 0; k < kLtK / 16; ++k)
-            umma_bf16_pair(d, lt_desc(a0, a_mn, k), lt_desc(b0, b_mn, k), idesc, kc > k_begin || k > 0);
-          umma_commit_pair(&bars->empty[s], leader);
+            for (int k = 0; k < kLtK / 16; ++k)
+              umma_bf16_pair(d, lt_desc(a0, a_mn, k), lt_desc(b0, b_mn, k), idesc, kc > k0 || k > 0);
+            umma_commit_pair(&bars->empty[s], leader);
+          }
+          if (dead) break;
+          umma_commit_pair(&bars->acc_full[ab], leader);
         }
-        if (dead) break;
-        umma_commit_pair(&bars->acc_full[ab], leader);
       }
       if (dead) {
         if (status) atomicOr(status, kDevTimeout);
@@ -422,12 +435,43 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
     for (int tile = pair; tile < tiles && !dead; tile += n_pairs, ++t) {
       const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
-      const uint32_t ab = t & 1;
       const int row0 = tm * 256 + (int)rank * 128 + q * 32, row = row0 + lane;
       if (fetch && !SPLIT) fetch_residual(way, &map_res, lane, tn * sh.bn + part * 32, row0);      // while the MMAs run
-      if (!mbar_wait(&bars->acc_full[ab], (t >> 1) & 1, abort_flag)) { dead = true; break; }
-      tc_fence_after();
-      const uint32_t d = tmem_base + ab * 256 + ((uint32_t)(q * 32) << 16);
+      const uint32_t lanes = (uint32_t)(q * 32) << 16;
+      if constexpr (PROMOTE) {
+        // all segments but the last: this warp's blocks of 32 columns (part * 32 + 64 i on) are added up in registers;
+        // then they go back to where the last one's sums are, and the epilogue takes them from there
+        float sum[4][32];
+        for (int g = 0; g < segments; ++g, ++t) {
+          const uint32_t ab = t & 1;
+          if (!mbar_wait(&bars->acc_full[ab], (t >> 1) & 1, abort_flag)) { dead = true; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int c = part * 32 + 64 * i;
+            if (c < sh.bn) {
+              float v[32];
+              tmem_ld32(tmem_base + ab * 256 + lanes + c, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) sum[i][j] = g == 0 ? v[j] : sum[i][j] + v[j];
+              if (g == segments - 1) tmem_st32(tmem_base + ab * 256 + lanes + c, sum[i]);
+            }
+          }
+          if (g == segments - 1) {
+            tmem_st_wait();
+            break;
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&bars->acc_empty[ab]), leader));
+        }
+        if (dead) break;
+      } else {
+        if (!mbar_wait(&bars->acc_full[t & 1], (t >> 1) & 1, abort_flag)) { dead = true; break; }
+        tc_fence_after();
+      }
+      const uint32_t ab = t & 1, d = tmem_base + ab * 256 + lanes;
       if (SPLIT) {         // partial sums to this block's shared memory (the pipeline's, idle by now), four columns a piece
         float4* mine = reinterpret_cast<float4*>(smem) + q * 32 + lane;
         for (int c = part * 32; c < sh.bn; c += 64) {
@@ -590,6 +634,19 @@ __device__ __forceinline__ void columns_out(const LinEpilogue& e, const LtShape&
 __host__ __device__ __forceinline__ int split_share(int bn, int split) { return (bn / 4 + split - 1) / split * 4; }
 __host__ __device__ __forceinline__ uint32_t split_room(int bn, int split) { return split > 1 ? (uint32_t)split_share(bn, split) * split * 512u : 0u; }
 
+// 16 columns of tensor memory, summed over the accumulators `stride` columns apart in their order
+__device__ __forceinline__ void tmem_sum16(uint32_t at, int accs, int stride, float* v) {
+  tmem_ld16(at, v);
+  tmem_ld_wait();
+  for (int a = 1; a < accs; ++a) {
+    float w[16];
+    tmem_ld16(at + a * stride, w);
+    tmem_ld_wait();
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] += w[j];
+  }
+}
+
 // map_l: the operand indexed by D's columns (accumulator lanes), map_r: the one indexed by D's rows.
 template <int KIND>
 __global__ void __launch_bounds__(kLtSplitThreads)
@@ -609,8 +666,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
   const int part = (int)(blockIdx.x % split), tile = (int)(blockIdx.x / split);
   const int tn = tile % sh.tiles_n, tm = tile / sh.tiles_n;
   const int k_begin = (int)((int64_t)sh.kchunks * part / split), k_end = (int)((int64_t)sh.kchunks * (part + 1) / split);
+  const int accs = sh.accs;                // accumulators beside one another, each for a run of the stages (see kLtSegment)
+  const int run = (k_end - k_begin + accs - 1) / accs;
   int cols_tmem = 32;
-  while (cols_tmem < sh.bn) cols_tmem *= 2;
+  while (cols_tmem < sh.bn * accs) cols_tmem *= 2;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < sh.stages; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
@@ -661,16 +720,17 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
   } else if (warp == 1) {
     if (lane == 0) {
       const uint32_t idesc = umma_idesc_bf16_any(128, sh.bn, l_mn, r_mn);
-      uint32_t it = 0;
-      for (int kc = k_begin; kc < k_end; ++kc, ++it) {
+      uint32_t it = 0, acc = tmem_base;
+      for (int kc = k_begin, in_run = 0; kc < k_end; ++kc, ++it) {
         const int s = it % sh.stages;
         if (!mbar_wait(&bars->full[s], (it / sh.stages) & 1, abort_flag)) { dead = true; break; }
         tc_fence_after();
         const uint32_t l0 = smem_u32(smem + (size_t)s * stage_bytes), r0 = l0 + 2 * kLtBox;
 #pragma unroll
         for (int k = 0; k < kLtK / 16; ++k)
-          umma_bf16(tmem_base, lt_desc(l0, l_mn, k), lt_desc(r0, r_mn, k), idesc, (kc > k_begin || k > 0) ? 1u : 0u);
+          umma_bf16(acc, lt_desc(l0, l_mn, k), lt_desc(r0, r_mn, k), idesc, (in_run > 0 || k > 0) ? 1u : 0u);
         umma_commit(&bars->empty[s]);
+        if (++in_run == run) { in_run = 0; acc += sh.bn; }
       }
       umma_commit(&bars->acc_full[0]);       // on the way out of a dead loop too: MMAs in flight have to finish
       if (dead) {
@@ -691,6 +751,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
   const int col = tn * 128 + q * 32 + lane;
   const float bias = KIND == kEpiForward && epi.bias && col < sh.N ? epi.bias[col] : 0.f;
   const int64_t row0 = (int64_t)tm * sh.bn;
+  const int used = (k_end - k_begin + run - 1) / run;          // accumulators that hold something
   if (split == 1) {
     if (warp >= 2) {
       for (int c = 0; c < sh.bn && !dead && row0 + c < sh.M; c += 16) {
@@ -699,8 +760,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
         __syncwarp();
         if (c == 0 && !mbar_wait(&bars->acc_full[0], 0, abort_flag)) { dead = true; break; }
         tc_fence_after();
-        tmem_ld16(d + c, v);
-        tmem_ld_wait();
+        tmem_sum16(d + c, used, sh.bn, v);
         columns_out<KIND, 16>(epi, sh, v, aux, row0 + c, sh.M, col, bias, lane);
         __syncwarp();
       }
@@ -724,8 +784,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_cons
       int owner = 0, at = 0;                    // row c of the tile is row `at` of block `owner`'s
       for (int c = 0; c < sh.bn && !dead && row0 + c < sh.M; c += 16) {
         float v[16];
-        tmem_ld16(d + c, v);
-        tmem_ld_wait();
+        tmem_sum16(d + c, used, sh.bn, v);
 #pragma unroll
         for (int j = 0; j < 16; j += 4) {
           st_shared_cluster4(map_to_rank(to, owner) + at / 4 * 2048, v[j], v[j + 1], v[j + 2], v[j + 3]);
@@ -841,12 +900,16 @@ const Device* device() {
   if (cudaDeviceGetAttribute(&n.n_sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n.n_sm < 2) return nullptr;
   const int pair = (int)kPairSmem, split = (int)kSplitSmemMax;
   const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  if (cudaFuncSetAttribute(linear_pair_kernel<kEpiForward, false>, at, pair) != cudaSuccess ||
-      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, false>, at, pair) != cudaSuccess ||
-      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, false>, at, pair) != cudaSuccess ||
-      cudaFuncSetAttribute(linear_pair_kernel<kEpiForward, true>, at, pair) != cudaSuccess ||
-      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, true>, at, pair) != cudaSuccess ||
-      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, true>, at, pair) != cudaSuccess ||
+  if (cudaFuncSetAttribute(linear_pair_kernel<kEpiForward, false, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, false, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, false, true>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, false, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, false, true>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiForward, true, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, true, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiInput, true, true>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, true, false>, at, pair) != cudaSuccess ||
+      cudaFuncSetAttribute(linear_pair_kernel<kEpiWeight, true, true>, at, pair) != cudaSuccess ||
       cudaFuncSetAttribute(linear_split_kernel<kEpiForward>, at, split) != cudaSuccess ||
       cudaFuncSetAttribute(linear_split_kernel<kEpiInput>, at, split) != cudaSuccess ||
       cudaFuncSetAttribute(linear_split_kernel<kEpiWeight>, at, split) != cudaSuccess)
@@ -855,7 +918,7 @@ const Device* device() {
     cudaLaunchAttribute attr[2] = {};
     cudaLaunchConfig_t cfg = config(2u * k, kLtPairThreads, kPairSmem, 2u * k, attr, nullptr);
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n.clusters[k], linear_pair_kernel<kEpiForward, true>, &cfg) != cudaSuccess) return nullptr;
+    if (cudaOccupancyMaxActiveClusters(&n.clusters[k], linear_pair_kernel<kEpiForward, true, false>, &cfg) != cudaSuccess) return nullptr;
     if (n.clusters[k] < 1) n.clusters[k] = 1;
   }
   n.ready = true;
@@ -944,8 +1007,11 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
       if (rest) epi.db = nullptr;
       const cudaLaunchConfig_t cfg = config((unsigned)(2 * pairs), kLtPairThreads, kPairSmem, 2u * split, attr, s);
       ++g_kernel_launches;
-      return split > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, true>, a, b, o, r, sh, epi, split, (int)rest, status)
-                       : cudaLaunchKernelEx(&cfg, linear_pair_kernel<KIND, false>, a, b, o, r, sh, epi, 1, 0, status);
+      auto kernel = split > 1 ? linear_pair_kernel<KIND, true, false> : linear_pair_kernel<KIND, false, false>;
+      if constexpr (KIND != kEpiForward)
+        if (p.epi.out_f32 && up(sh.kchunks, split) > kLtSegment)
+          kernel = split > 1 ? linear_pair_kernel<KIND, true, true> : linear_pair_kernel<KIND, false, true>;
+      return cudaLaunchKernelEx(&cfg, kernel, a, b, o, r, sh, epi, split, (int)rest, status);
     };
     // The last wave of a launch that needs more than one is seldom full. It becomes a launch of its own with the contraction
     // split over two to four pairs a tile, which starts on the SMs the full waves leave, where the rounds that takes are
@@ -968,6 +1034,9 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
   } else {
     sh.tiles_m = (int)up(p.M, c.bn);
     sh.tiles_n = (int)up(p.N, 128);
+    // accumulators: as many as the stages call for and fit beside the other blocks of an SM in its 512 columns
+    const int64_t want = up(up(sh.kchunks, c.split), kLtSegment), fit = (c.bn <= 16 ? 128 : c.bn <= 64 ? 256 : 512) / c.bn;
+    sh.accs = (int)(want < fit ? want : fit);
     const int64_t blocks = (int64_t)sh.tiles_m * sh.tiles_n * c.split;
     if (blocks > 0x7fffffff) return SC_ERR_TOO_LARGE;
     if (!encode_operand(&a, p.A, p.M, p.K, c.bn) || !encode_operand(&b, p.B, p.N, p.K, 128)) return SC_ERR_CUDA;
