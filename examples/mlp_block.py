@@ -1,0 +1,96 @@
+"""A pre-norm MLP block trained with the library alone: layer norm, two linear layers, activations kept in 8 bits for the
+backward pass, masked weight gradients, and the spectrally corrected step that consumes them.
+
+    h = layer_norm(x)      z = h W1^T + b1      y = gelu(z) W2^T + b2 + x
+
+Between forward and backward the block keeps x, the row statistics and two checkpoints (h masked, z): 33 bytes for 32
+values instead of 64. Now and then an anchor gradient arrives (from an unmasked checkpoint of h, which the norm writes
+beside its output). The task is a fixed random block to imitate.
+
+    python examples/mlp_block.py [--hidden 1024] [--ffn 4096] [--tokens 2048] [--steps 40]
+"""
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2609_14339_b200 as sc  # noqa: E402
+
+
+class MlpBlock:
+    def __init__(self, hidden, ffn, seed=0, keep=0.25, rank=16, lr=2e-3, device="cuda:0"):
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+        self.keep, self.lr, self.seed = keep, lr, seed
+        self.W = [torch.randn((ffn, hidden), generator=g, device=device) * hidden ** -0.5,
+                  torch.randn((hidden, ffn), generator=g, device=device) * ffn ** -0.5]
+        self.Wb = [w.bfloat16() for w in self.W]                      # what the products read; the step rewrites them
+        self.b = [torch.zeros(ffn, device=device), torch.zeros(hidden, device=device)]
+        self.norm = [torch.ones(hidden, device=device), torch.zeros(hidden, device=device)]
+        self.m, self.v = [torch.zeros_like(w) for w in self.W], [torch.zeros_like(w) for w in self.W]
+        hp = sc.Hparams.default(lr=lr, alpha=0.5, tau_p=1e-4, grads_prescaled=1)
+        self.plan = sc.Plan([tuple(w.shape) for w in self.W], rank, keep, hp, device=device)
+        self.step = 0
+
+    def forward(self, x, anchor=False):
+        """y, and what the backward pass needs."""
+        tokens, hidden = x.shape
+        unmasked = sc.Act8.empty(tokens, hidden, x.device) if anchor else None
+        h, stats = sc.layer_norm(x, self.norm[0], self.norm[1], save=unmasked)
+        masked = sc.act8_compress(sc.apply_prf_mask(h, self.keep, self.seed, 0, self.step, rescale=False))
+        z = sc.Act8.empty(tokens, self.W[0].shape[0], x.device)
+        a = sc.linear(h, self.Wb[0], bias=self.b[0], act="gelu", save=z)
+        y = sc.linear(a, self.Wb[1], bias=self.b[1], residual=x)
+        return y, (x, stats, masked, z, unmasked)
+
+    def backward(self, dy, kept):
+        """Gradients of the weights (masked, rescaled), of the vectors and of x."""
+        x, stats, masked, z, unmasked = kept
+        G2, db2 = sc.linear_weight_grad(dy, z, act="gelu")
+        dz = sc.linear_backward_input(dy, self.Wb[1], saved=z, act="gelu")
+        G1, db1 = sc.linear_weight_grad(dz, masked, scale=1.0 / self.keep)
+        dh = sc.linear_backward_input(dz, self.Wb[0])
+        dx, dg, dc = sc.layer_norm_backward(dh, x, self.norm[0], stats, residual_grad=dy)
+        anchors = None
+        if unmasked is not None:
+            anchors = [sc.linear_weight_grad(dz, unmasked)[0], G2]
+        return [G1, G2], [db1, db2, dg, dc], dx, anchors
+
+    def update(self, grads, vector_grads, anchors):
+        self.step += 1
+        if anchors is not None:
+            self.plan.anchor_update(anchors, step_tag=self.step)
+        self.plan.correct_and_step(grads, self.W, self.m, self.v, step=self.step, params_bf16=self.Wb)
+        for p, g in zip(self.b + self.norm, vector_grads):
+            p.sub_(g, alpha=self.lr)
+
+
+def train(hidden=1024, ffn=4096, tokens=2048, steps=40, anchor_every=5, seed=0, device="cuda:0"):
+    """Mean squared error per step of a block that learns to imitate another."""
+    teacher, block = MlpBlock(hidden, ffn, seed=seed + 100, device=device), MlpBlock(hidden, ffn, seed=seed, device=device)
+    g = torch.Generator(device=device)
+    g.manual_seed(seed + 1)
+    losses = []
+    for step in range(steps):
+        x = torch.randn((tokens, hidden), generator=g, device=device).bfloat16()
+        target, _ = teacher.forward(x)
+        y, kept = block.forward(x, anchor=step % anchor_every == 0)
+        diff = y.float() - target.float()
+        losses.append((diff * diff).mean())
+        dy = (diff * (2.0 / diff.numel())).bfloat16()
+        grads, vectors, _, anchors = block.backward(dy, kept)
+        block.update(grads, vectors, anchors)
+    return [float(v) for v in torch.stack(losses).cpu()]
+
+
+if __name__ == "__main__":
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--hidden", type=int, default=1024)
+    ap.add_argument("--ffn", type=int, default=4096)
+    ap.add_argument("--tokens", type=int, default=2048)
+    ap.add_argument("--steps", type=int, default=40)
+    a = ap.parse_args()
+    for i, loss in enumerate(train(a.hidden, a.ffn, a.tokens, a.steps)):
+        print("step %3d  mse %.5f" % (i, loss))
