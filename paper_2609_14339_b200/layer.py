@@ -130,13 +130,17 @@ _KEEP = 16 << 20
 _workspaces = {}
 
 
-def _kept_workspace(device: int, queue: int, need: int) -> int:
-    """Workspace of at most _KEEP bytes, kept per stream: what is queued there uses it in turn."""
+def _workspace(device: int, queue: int, need: int):
+    """A workspace of at most _KEEP bytes is kept per stream: what is queued there uses it in turn. A larger one (the size
+    of an activation) goes back to the stream's pool, and a graph that is being captured gets its own, since it may be
+    replayed beside the stream's later work."""
+    if need > _KEEP or torch._C._cuda_isCurrentStreamCapturing():
+        return torch.empty((need,), dtype=_U8, device=torch.device("cuda", device))
     held = _workspaces.get((device, queue))
     if held is None or held.numel() < need:
         held = torch.empty((max(need, 1 << 20),), dtype=_U8, device=torch.device("cuda", device))
         _workspaces[(device, queue)] = held
-    return held.data_ptr()
+    return held
 
 
 class Act8:
@@ -217,12 +221,18 @@ def layer_norm_backward(dY, X, weight, stats, residual_grad=None, out=None, dwei
         out, lddx = X.new_empty((rows, cols)), cols
     else:
         lddx = _matrix("out", out, rows, cols, dt, dev)[2]
-    if dweight is None:
+    if dweight is None and dbias is None:
+        dweight, dbias = stats.new_empty((2, cols)).unbind(0)
+    elif dweight is None:
         dweight = stats.new_empty((cols,))
-    if dbias is None:
+    elif dbias is None:
         dbias = stats.new_empty((cols,))
     queue = _raw_stream(dev)
-    ws = _kept_workspace(dev, queue, need) if workspace is None else _buffer("workspace", workspace, need, dev)
+    if workspace is None:
+        workspace = _workspace(dev, queue, need)
+        ws = workspace.data_ptr()
+    else:
+        ws = _buffer("workspace", workspace, need, dev)
     _done(lib.sc_layernorm_backward(dY.data_ptr(), X.data_ptr(), _DTYPES[dt], w, st, r, out.data_ptr(),
                                     _vector("dweight", dweight, cols, dev), _vector("dbias", dbias, cols, dev), rows,
                                     cols, lddy, ldx, ldr, lddx, ws, need, queue), "sc_layernorm_backward")
@@ -353,13 +363,11 @@ def linear_weight_grad(dY, saved, act="none", scale: float = 1.0, out=None, out_
     if dbias is None:
         dbias = dY.new_empty((rows,), dtype=_F32)
     queue = _raw_stream(dev)
-    if workspace is not None:
-        ws = _buffer("workspace", workspace, need, dev)
-    elif need <= _KEEP:
-        ws = _kept_workspace(dev, queue, need)
-    else:                                   # the size of an activation: goes back to the stream's pool
-        workspace = dY.new_empty((need,), dtype=_U8)
+    if workspace is None:
+        workspace = _workspace(dev, queue, need)
         ws = workspace.data_ptr()
+    else:
+        ws = _buffer("workspace", workspace, need, dev)
     _done(lib.sc_linear_weight_grad(dY.data_ptr(), _DTYPES[dt], a8, a, scale, out.data_ptr(), _DTYPES[odt],
                                     _vector("dbias", dbias, rows, dev), tokens, rows, cols, lddy, ws, need,
                                     _status(status, dev), queue), "sc_linear_weight_grad")
