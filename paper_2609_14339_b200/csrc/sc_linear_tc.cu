@@ -9,6 +9,11 @@
 //                       accumulator lanes, so that a tile of few rows wastes nothing), the contraction split over a cluster
 //                       of up to 8 blocks, joined the same way.
 //
+// Full chip, the pair kernel is bound by what an SM takes in: 32 KB a stage of 64 terms in 560 to 660 clocks, of 512 that its
+// MMAs take (2048 x 8192 x 2048: 55 us, 1260 TFLOP/s; torch's product 52); large products by the power limit (4096 x 4096 x
+// 14336: 1.40 GHz of 1.97, 402 us, torch's 394). The split kernel is bound by HBM and the first loads' way (1 x 14336 x
+// 4096: 23 us, 5.1 TB/s).
+//
 // Operands come by TMA in boxes of 64 along k, 128-byte swizzle; an operand whose contraction index is slow in memory is
 // taken as it lies (MN-major descriptor), nothing is transposed. Sizes that end inside a box come in as zeros.
 // Every mbarrier wait is bounded; a wait that runs out latches the time-out bit in *status and the block winds down.
@@ -123,15 +128,27 @@ __device__ __forceinline__ void epilogue_value32(const LinEpilogue& e, const LtS
     for (int j = 0; j < 32; ++j) v[j] *= e.scale;
   }
 }
-// what the epilogue needs besides the sums, read before the sums are waited for: slopes of the checkpoint
+// A row's block of a checkpoint, as it lies. Asked for one block ahead, the first one before a tile's sums are waited for
+// (input gradient with SiLU, 2048 x 2048 x 8192: 59.6 us, 61.9 when each block is asked for as it is needed).
+struct SavedBlock {
+  uint4 a, b;
+  uint32_t e;
+};
 template <int KIND>
-__device__ __forceinline__ void epilogue_aux32(const LinEpilogue& e, const LtShape& sh, float* aux, int64_t row, int col) {
-  if (KIND == kEpiInput && e.q) {
+__device__ __forceinline__ void saved_load(const LinEpilogue& e, const LtShape& sh, SavedBlock& s, int64_t row, int col) {
+  if (KIND == kEpiInput && e.q && row < sh.M && col < sh.N) {
     const uint4* q = reinterpret_cast<const uint4*>(e.q + a8_at(sh.M, row, col));
-    const uint4 a = q[0], b = q[1];
-    const float step = a8_step(e.e[a8_scale_at(sh.M, row, col)]);
-    a8_unpack4(a.x, step, aux); a8_unpack4(a.y, step, aux + 4); a8_unpack4(a.z, step, aux + 8); a8_unpack4(a.w, step, aux + 12);
-    a8_unpack4(b.x, step, aux + 16); a8_unpack4(b.y, step, aux + 20); a8_unpack4(b.z, step, aux + 24); a8_unpack4(b.w, step, aux + 28);
+    s.a = q[0];
+    s.b = q[1];
+    s.e = e.e[a8_scale_at(sh.M, row, col)];
+  }
+}
+template <int KIND>
+__device__ __forceinline__ void saved_slopes(const LinEpilogue& e, const SavedBlock& s, float* aux) {
+  if (KIND == kEpiInput && e.q) {
+    const float step = a8_step(s.e);
+    a8_unpack4(s.a.x, step, aux); a8_unpack4(s.a.y, step, aux + 4); a8_unpack4(s.a.z, step, aux + 8); a8_unpack4(s.a.w, step, aux + 12);
+    a8_unpack4(s.b.x, step, aux + 16); a8_unpack4(s.b.y, step, aux + 20); a8_unpack4(s.b.z, step, aux + 24); a8_unpack4(s.b.w, step, aux + 28);
     act_slopes<32>(e.act, aux);
   }
 }
@@ -343,6 +360,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int q = warp & 3, part = (warp - 2) >> 2;      // epilogue warps: quarter of the lanes; every second 32 columns
   WayOut way{staging + (warp - 2) * kLtStaging, &bars->res[(warp - 2) & 7], 0u};
   const bool fetch = KIND == kEpiForward && epi.res && sh.staged;
+  SavedBlock early{};
+  // split contraction: this warp's blocks of 32 columns, every second one of this pair's share
+  const int first = SPLIT ? sh.bn / 32 * part_k / split + part : 0, last = SPLIT ? sh.bn / 32 * (part_k + 1) / split : 0;
   bool dead = false;
   if (warp == 0) {
     if (lane == 0) {
@@ -437,6 +457,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       const int tm = sh.m_fastest ? tile % sh.tiles_m : tile / sh.tiles_n, tn = sh.m_fastest ? tile / sh.tiles_m : tile % sh.tiles_n;
       const int row0 = tm * 256 + (int)rank * 128 + q * 32, row = row0 + lane;
       if (fetch && !SPLIT) fetch_residual(way, &map_res, lane, tn * sh.bn + part * 32, row0);      // while the MMAs run
+      SavedBlock saved{};
+      if (SPLIT && !PROMOTE) saved_load<KIND>(epi, sh, early, row, tn * sh.bn + first * 32);
+      if (!SPLIT && !PROMOTE) saved_load<KIND>(epi, sh, saved, row, tn * sh.bn + part * 32);
       const uint32_t lanes = (uint32_t)(q * 32) << 16;
       if constexpr (PROMOTE) {
         // all segments but the last: this warp's blocks of 32 columns (part * 32 + 64 i on) are added up in registers;
@@ -467,6 +490,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&bars->acc_empty[ab]), leader));
         }
         if (dead) break;
+        if (!SPLIT) saved_load<KIND>(epi, sh, saved, row, tn * sh.bn + part * 32);     // earlier it would take the sums' registers
       } else {
         if (!mbar_wait(&bars->acc_full[t & 1], (t >> 1) & 1, abort_flag)) { dead = true; break; }
         tc_fence_after();
@@ -486,7 +510,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           const int col = tn * sh.bn + c;
           const bool live = row < sh.M && col < sh.N;
           float v[32], aux[32];
-          if (live) epilogue_aux32<KIND>(epi, sh, aux, row, col);
+          saved_slopes<KIND>(epi, saved, aux);
+          if (c + 64 < sh.bn) saved_load<KIND>(epi, sh, saved, row, col + 64);
           __syncwarp();
           tmem_ld32(d + c, v);
           tmem_ld_wait();
@@ -508,10 +533,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   }
   if (SPLIT) {
     // join: each pair finishes its share of the tile's blocks of 32 columns, adding the pairs' sums in their order
+    const int tm = sh.m_fastest ? pair % sh.tiles_m : pair / sh.tiles_n, tn = sh.m_fastest ? pair / sh.tiles_m : pair % sh.tiles_n;
+    const int row0 = tm * 256 + (int)rank * 128 + q * 32, row = row0 + lane;
     __syncwarp();
     cluster_sync_all();
     if (warp >= 2) {
-      const int tm = sh.m_fastest ? pair % sh.tiles_m : pair / sh.tiles_n, tn = sh.m_fastest ? pair / sh.tiles_m : pair % sh.tiles_n;
+      SavedBlock saved = early;
+      if (PROMOTE && first < last) saved_load<KIND>(epi, sh, saved, row, tn * sh.bn + first * 32);
       if (KIND == kEpiWeight && epi.db && part_k == 0) {
         const int g = bias_share(sh.tiles_n), c = threadIdx.x - 64;
         const int64_t col = tm * 256 + (int)rank * 128 + tn * g * 8 + c;
@@ -521,14 +549,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           epi.db[col] = v;
         }
       }
-      const int row0 = tm * 256 + (int)rank * 128 + q * 32, row = row0 + lane, blocks = sh.bn / 32;
-      const int last = blocks * (part_k + 1) / split;
-      for (int blk = blocks * part_k / split + part; blk < last && !dead; blk += 2) {
+      for (int blk = first; blk < last && !dead; blk += 2) {
         const int col = tn * sh.bn + blk * 32;
         const bool live = row < sh.M && col < sh.N;
         float v[32], aux[32];
         if (fetch) fetch_residual(way, &map_res, lane, col, row0);
-        if (live) epilogue_aux32<KIND>(epi, sh, aux, row, col);
+        saved_slopes<KIND>(epi, saved, aux);
+        if (blk + 2 < last) saved_load<KIND>(epi, sh, saved, row, col + 64);
         const uint32_t at = smem_u32(smem) + (uint32_t)(blk * 8 * 128 + q * 32 + lane) * 16;
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = 0.f;
