@@ -36,7 +36,7 @@ constexpr int kLtStaging = 4096;              // per epilogue warp: two 32 x 32 
 // (4.4e-6 after 4096 terms of random sign, 1.4e-5 of one sign). A bf16 result does not show that, an fp32 gradient summed
 // over many tokens does: its accumulators are added up in fp32 after every kLtSegment stages at most (768 terms; 16384
 // tokens: 1.9e-5 off without, 1.4e-7 with). For pairs of SMs that costs time, since reading 128 KB of accumulators beside
-// the MMAs takes about as long as 12 stages (2048 x 8192 x 2048: 58 us without, 68 with), so it is left to fp32 gradients;
+// the MMAs takes about as long as 12 stages (2048 x 8192 x 2048: 53 us without, 64 with), so it is left to fp32 gradients;
 // the forward product does without whatever its result's type, so that the type and a checkpoint change nothing in its
 // sums. With few rows several accumulators fit beside one another and cost nothing.
 constexpr int kLtSegment = 12;
@@ -52,7 +52,7 @@ struct LtShape {
   int m_fastest;           // pair: which way consecutive tiles run
   int stages, accs;        // split
   int vec;                 // out and res take 16-byte accesses
-  int staged;              // pair: bf16 out (and res) that TMA can describe; the epilogue goes through shared memory
+  int staged;              // pair: out (and res) that TMA can describe; the epilogue goes through shared memory
   int vec_bias;
 };
 
@@ -157,7 +157,9 @@ __device__ __forceinline__ void saved_slopes(const LinEpilogue& e, const SavedBl
 // are four pieces of 16, and the 4096 pieces of a block's 128 x 256 bf16 results took 6000 clocks, a quarter of a tile
 // with 2048 terms, the shared-memory pipe shared with the tensor core's operands meanwhile. So bf16 blocks go through two
 // 2 KB buffers per warp (64-byte swizzle: no two of 8 rows in one bank) and out by TMA, which cuts off what lies outside;
-// a residual comes in the same way, before the sums are waited for, and is added in place.
+// a residual comes in the same way, before the sums are waited for, and is added in place. An fp32 block leaves as two of
+// 32 x 16, of the same layout (weight gradient of 4096 x 14336 from 4096 tokens 409 us, 453 stored from the registers; from
+// 2 tokens 56 and 124). fp32 results with a residual take the registers' way.
 struct WayOut {
   uint8_t* buf;              // this warp's two buffers
   uint64_t* bar;             // residual landed
@@ -193,6 +195,26 @@ __device__ __forceinline__ bool way_out(WayOut& w, const LinEpilogue& e, const L
 #pragma unroll
       for (int j = 0; j < 32; j += 8)
         if (j < left) store8(e.out, e.out_f32, (int64_t)row * e.ldo + col + j, sh.vec, left - j, v + j);
+    }
+    return true;
+  }
+  if (e.out_f32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint8_t* buf = w.buf + h * 2048;
+      if (lane == 0) tma_store_wait_read<1>();
+      __syncwarp();
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float* x = v + 16 * h + 4 * p;
+        *staged_piece(buf, lane, p) = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        if (row0 < sh.M && left > 16 * h) tma_store_2d(map_out, buf, col + 16 * h, row0);
+        tma_store_commit();
+      }
     }
     return true;
   }
@@ -869,16 +891,16 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-// outer x inner bf16 matrix -> boxes of 64 (inner) x box_outer, 128-byte swizzle
+// outer x inner bf16 (or fp32) matrix -> boxes of 64 (inner) x box_outer, 128-byte swizzle
 bool encode(CUtensorMap* out, const void* base, int64_t inner, int64_t outer, int64_t ld, int box_outer, int box_inner = 64,
-            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
+            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B, bool f32 = false) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
   cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-  cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+  cuuint64_t strides[1] = {(cuuint64_t)ld * (f32 ? 4 : 2)};
   cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
   cuuint32_t estr[2] = {1, 1};
-  return enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+  return enc(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -1020,9 +1042,10 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
     sh.m_fastest = p.M <= p.N;
     if (!encode_operand(&a, p.A, p.M, p.K, 128) || !encode_operand(&b, p.B, p.N, p.K, c.bn / 2)) return SC_ERR_CUDA;
     CUtensorMap o = a, r = a;          // placeholders where the epilogue does not go through shared memory
-    sh.staged = sh.vec && !p.epi.out_f32;
+    sh.staged = sh.vec && !(p.epi.out_f32 && p.epi.res);
     if (sh.staged) {
-      if (!encode(&o, p.epi.out, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return SC_ERR_CUDA;
+      if (!encode(&o, p.epi.out, p.N, p.M, p.epi.ldo, 32, p.epi.out_f32 ? 16 : 32, CU_TENSOR_MAP_SWIZZLE_64B, p.epi.out_f32))
+        return SC_ERR_CUDA;
       if (p.epi.res && !encode(&r, p.epi.res, p.N, p.M, p.epi.ldr, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return SC_ERR_CUDA;
     }
     const int slots = dev->n_sm / 2;
