@@ -69,25 +69,32 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 // A thread's EPT columns of one row, as they lie in memory. VEC: pieces of 16 bytes, neighbouring threads' pieces beside
 // one another (the number of columns is a multiple of a piece, so a piece is inside the row or outside); otherwise every
-// blockDim-th column, one at a time (any stride, alignment and width, still coalesced). Outside the row: zeros.
-template <bool F32, int EPT, bool VEC>
+// THREADS-th column, one at a time (any stride, alignment and width, still coalesced). Outside the row: zeros. Places are a
+// thread's first one plus constants: computed from the block's run-time size, they were half of all instructions of single
+// columns (16384 x 4001 bf16: 190 and 358 us forward and backward, now 127 and 185). THREADS 0: the run-time size all the
+// same, in fp32 kernels of 1024 threads and whole pieces, whose 64 registers the constants overflow (16384 x 8192: 170 and
+// 342 us forward and backward, with constants 175 and 377).
+__host__ __device__ constexpr int block_of(bool f32_pieces, int threads) { return f32_pieces && threads == 1024 ? 0 : threads; }
+template <bool F32, int EPT, bool VEC, int THREADS>
 struct Piece {
   static constexpr int kPiece = F32 ? 4 : 8;          // columns in 16 bytes
   static constexpr int kWords = EPT * (F32 ? 4 : 2) / 4;
   uint32_t w[VEC ? kWords : EPT];
-  __device__ static int col(int i) {
-    return VEC ? (i / kPiece * (int)blockDim.x + (int)threadIdx.x) * kPiece + i % kPiece : (int)threadIdx.x + i * (int)blockDim.x;
-  }
+  __device__ static int threads() { return THREADS ? THREADS : (int)blockDim.x; }
+  __device__ static int base() { return (int)threadIdx.x * (VEC ? kPiece : 1); }
+  __device__ static int ahead(int i) { return VEC ? i / kPiece * threads() * kPiece + i % kPiece : i * threads(); }
+  __device__ static int col(int i) { return base() + ahead(i); }
   __device__ static bool in(int i, int cols) { return col(VEC ? i / kPiece * kPiece : i) < cols; }
   // columns of a row that the block's warp `warp` holds
   __device__ static float columns_of(int warp, int cols) {
     constexpr int kRun = VEC ? kPiece : 1;
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < EPT; i += kRun) c += min(32 * kRun, max(0, cols - i * (int)blockDim.x - warp * 32 * kRun));
+    for (int i = 0; i < EPT; i += kRun) c += min(32 * kRun, max(0, cols - i * threads() - warp * 32 * kRun));
     return (float)c;
   }
   __device__ void load(const void* p, int64_t at, int cols) {
+    const char* from = static_cast<const char*>(p) + (at + base()) * (F32 ? 4 : 2);
     if (VEC) {
 #pragma unroll
       for (int k = 0; k < kWords / 4; ++k) {
@@ -97,7 +104,7 @@ struct Piece {
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) w[i] = in(i, cols) ? __float_as_uint(ld1<F32>(p, at + col(i))) : 0u;
+      for (int i = 0; i < EPT; ++i) w[i] = in(i, cols) ? __float_as_uint(ld1<F32>(from, ahead(i))) : 0u;
     }
   }
   __device__ f2 pair(int i) const { return f2_make(get(2 * i), get(2 * i + 1)); }
@@ -106,21 +113,22 @@ struct Piece {
     return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
 };
-template <bool F32, int EPT, bool VEC>
+template <bool F32, int EPT, bool VEC, int THREADS>
 __device__ __forceinline__ void store_piece(void* p, int64_t at, int cols, const float* v) {
-  typedef Piece<F32, EPT, VEC> P;
+  typedef Piece<F32, EPT, VEC, THREADS> P;
+  char* to = static_cast<char*>(p) + (at + P::base()) * (F32 ? 4 : 2);
   if (VEC) {
 #pragma unroll
     for (int i = 0; i < EPT; i += P::kPiece) {
       if (P::in(i, cols)) {
         if (F32) *reinterpret_cast<float4*>(static_cast<float*>(p) + at + P::col(i)) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-        else store8(p, 0, at + P::col(i), true, 8, v + i);
+        else store8(to, 0, P::ahead(i), true, 8, v + i);
       }
     }
   } else {
 #pragma unroll
     for (int i = 0; i < EPT; ++i)
-      if (P::in(i, cols)) st1<F32>(p, at + P::col(i), v[i]);
+      if (P::in(i, cols)) st1<F32>(to, P::ahead(i), v[i]);
   }
 }
 
@@ -184,7 +192,8 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
                     int cols, int64_t ldx, int64_t ldy) {
   extern __shared__ float4 forward_smem[];
   __shared__ float2 red[2][2][32];
-  typedef Piece<F32, EPT, VEC> P;
+  constexpr int kBlock = block_of(F32 && VEC, THREADS);
+  typedef Piece<F32, EPT, VEC, kBlock> P;
   typedef Params<EPT, THREADS> W;
   constexpr bool RING = EPT == 16;
   constexpr int ROWS = 2, WARPS = THREADS / 32;
@@ -337,7 +346,7 @@ norm_forward_kernel(const void* X, const float* __restrict__ weight, const float
           }
         }
       }
-      store_piece<F32, EPT, VEC>(Y, r * ldy, cols, y);
+      store_piece<F32, EPT, VEC, kBlock>(Y, r * ldy, cols, y);
     }
   }
 }
@@ -351,7 +360,8 @@ norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ we
   extern __shared__ uint4 ring_smem[];
   __shared__ float red[2][2][32];
   __shared__ Params<EPT, THREADS> pw;
-  typedef Piece<F32, EPT, VEC> P;
+  constexpr int kBlock = block_of(F32 && VEC && EPT == 8, THREADS);
+  typedef Piece<F32, EPT, VEC, kBlock> P;
   // 16 bf16 columns a thread: two rows on their way through shared memory (one row, 48 KB per SM, in registers: 5.0 TB/s
   // for 16384 x 8192). Else the next row in registers, as far as they go.
   constexpr bool RING = !F32 && VEC && EPT == 16;
@@ -449,7 +459,7 @@ norm_backward_kernel(const void* dY, const void* X, const float* __restrict__ we
         v[2 * i] = o.x; v[2 * i + 1] = o.y;
       }
     }
-    store_piece<F32, EPT, VEC>(dX, r * lddx, cols, v);
+    store_piece<F32, EPT, VEC, kBlock>(dX, r * lddx, cols, v);
   }
   if (part) {
 #pragma unroll
@@ -691,8 +701,8 @@ void backward_rows(const Backward& f, bool vec, cudaStream_t s) {
     const bool pieces = vec && f.cols % 4 == 0, narrow = f.cols <= 4096;
     if (pieces && narrow) by_threads<true, 4, true>(row_threads(f.cols, 4), go, s);
     else if (narrow) by_threads<true, 4, false>(row_threads(f.cols, 4), go, s);
-    else if (pieces) by_threads<true, 8, true>(row_threads(f.cols, 8), go, s);
-    else by_threads<true, 8, false>(row_threads(f.cols, 8), go, s);
+    else if (pieces) go.template go<true, 8, true, 1024>(s);
+    else go.template go<true, 8, false, 1024>(s);
   } else {
     if (vec && f.cols % 8 == 0) by_threads<false, 16, true>(row_threads(f.cols, 16), go, s);
     else by_threads<false, 8, false>(row_threads(f.cols, 8), go, s);
