@@ -10,9 +10,10 @@
 //                       of up to 8 blocks, joined the same way.
 //
 // Full chip, the pair kernel is bound by what an SM takes in: 32 KB a stage of 64 terms in 560 to 660 clocks, of 512 that its
-// MMAs take (2048 x 8192 x 2048: 55 us, 1260 TFLOP/s; torch's product 52); large products by the power limit (4096 x 4096 x
-// 14336: 1.40 GHz of 1.97, 402 us, torch's 394). The split kernel is bound by HBM and the first loads' way (1 x 14336 x
-// 4096: 23 us, 5.1 TB/s).
+// MMAs take (2048 x 8192 x 2048: 60 us, 1150 TFLOP/s; a library product takes 58), and by whole waves of tiles (4096 x 4096
+// x 14336: 354 us, 1360 TFLOP/s, in 3.67 waves of 3.46, library 319; 896 tiles of 4096 x 14336 x 4096: 324, library 337);
+// run on and on, by the power limit (388 to 402 us at 1.3 to 1.4 GHz of 1.97). The split kernel is bound by HBM and the
+// first loads' way (1 x 14336 x 4096: 23 us, 5.1 TB/s).
 //
 // Operands come by TMA in boxes of 64 along k, 128-byte swizzle; an operand whose contraction index is slow in memory is
 // taken as it lies (MN-major descriptor), nothing is transposed. Sizes that end inside a box come in as zeros.
