@@ -988,10 +988,14 @@ Choice choose(int kind, int64_t M, int64_t N, int64_t K, const Device& d) {
   const int64_t chunks = up(K, kLtK);
   Choice best;
   const int64_t lane_tiles = up(N, 128);
-  // Up to 128 rows the split kernel, unless they are more than 64 and its tiles fill the chip anyway: the pair kernel's
-  // epilogue then wins (128 x 14336 x 4096: 31 against 33 us, with a residual 34 against 54; 80 x 4096 x 4096 the other way
-  // round: 19 against 15).
-  if (M > 128 || (M > 64 && 4 * lane_tiles >= 3 * d.n_sm)) {
+  // Up to 64 rows the split kernel. With 65 to 128 a block of it fills an SM: it is the better one where its clusters of
+  // four all run at once (3968 columns: 33 such clusters fit a B200; 65 x 3968 x 4096 13.2 against 17.0 us, 128 rows 15.1
+  // against 17.3), or its clusters of two do and nearly fill the chip (65 x 9216 x 4096 21.8 against 27.4). Otherwise a second
+  // round of clusters, or idle SMs, cost more than the pair kernel's half-empty tiles: 128 x 5120 x 4096 19 us, 29 with
+  // clusters of four, 24 of two; 128 x 12696 x 14336 83 against 109; 128 x 14336 x 4096 31 against 33.
+  const int64_t fours = d.clusters[2], twos = d.clusters[1];
+  const bool by_four = lane_tiles <= fours, by_two = lane_tiles <= twos && 10 * lane_tiles >= 9 * twos;
+  if (M > 128 || (M > 64 && !by_four && !by_two)) {
     for (int bn = 256; bn >= 128; bn -= 32) {
       const int64_t tiles = up(M, 256) * up(N, bn);
       const double stage = 500.0 + bn;
@@ -1008,10 +1012,10 @@ Choice choose(int kind, int64_t M, int64_t N, int64_t K, const Device& d) {
   const int bn = (int)up(M, step) * step;
   const size_t stage_bytes = 2 * kLtBox + (size_t)bn * 128;
   // Enough blocks for every SM, two of them side by side (1 x 14336 x 4096: 224 of four stages 24.2 us, 112 of six 28.5): one's
-  // loads cover another's join. More than 64 rows leave room for one, with clusters of up to four: of eight the chip takes
-  // few at a time.
+  // loads cover another's join. More than 64 rows leave room for one, with clusters as above: of eight the chip takes few at a
+  // time.
   int split = 1;
-  while (split < (bn <= 64 ? 8 : 4) && lane_tiles * split < d.n_sm && 2 * split <= chunks) split *= 2;
+  while (split < (bn <= 64 ? 8 : by_four ? 4 : 2) && lane_tiles * split < d.n_sm && 2 * split <= chunks) split *= 2;
   const size_t budget = (size_t)(bn <= 16 ? 84 : bn <= 64 ? 110 : 220) * 1024;
   int stages = (int)((budget - split_room(bn, split)) / stage_bytes);
   if (stages > kLtMaxStages) stages = kLtMaxStages;
