@@ -54,7 +54,6 @@ struct LtShape {
   int stages, accs;        // split
   int vec;                 // out and res take 16-byte accesses
   int staged;              // pair: out (and res) that TMA can describe; the epilogue goes through shared memory
-  int ragged;              // staged, and a row of out ends inside 16 bytes
   int vec_bias;
 };
 
@@ -159,7 +158,7 @@ __device__ __forceinline__ void saved_slopes(const LinEpilogue& e, const SavedBl
 // are four pieces of 16, and the 4096 pieces of a block's 128 x 256 bf16 results took 6000 clocks, a quarter of a tile
 // with 2048 terms, the shared-memory pipe shared with the tensor core's operands meanwhile. So bf16 blocks go through two
 // 2 KB buffers per warp (64-byte swizzle: no two of 8 rows in one bank) and out by TMA, which cuts off what lies outside
-// in whole pieces of 16 bytes: where a row ends inside one, its last block is stored from the registers after all;
+// in whole pieces of 16 bytes, so an output whose rows end inside one takes the registers' way;
 // a residual comes in the same way, before the sums are waited for, and is added in place. An fp32 block leaves as two of
 // 32 x 16, of the same layout (weight gradient of 4096 x 14336 from 4096 tokens 409 us, 453 stored from the registers; from
 // 2 tokens 56 and 124). fp32 results with a residual take the registers' way.
@@ -179,14 +178,6 @@ __device__ __forceinline__ void fetch_residual(WayOut& w, const CUtensorMap* map
     tma_load_2d(w.buf + (w.n & 1) * 2048, map, w.bar, col, row);
   }
 }
-// a thread's row of the block, from the registers
-__device__ __forceinline__ void store_row32(const LinEpilogue& e, const LtShape& sh, const float* v, int row, int col) {
-  const int left = sh.N - col;
-  if (row >= sh.M) return;
-#pragma unroll
-  for (int j = 0; j < 32; j += 8)
-    if (j < left) store8(e.out, e.out_f32, (int64_t)row * e.ldo + col + j, sh.vec, left - j, v + j);
-}
 // row0: the block's first row. Called by whole warps; false: a wait ran out.
 template <int KIND>
 __device__ __forceinline__ bool way_out(WayOut& w, const LinEpilogue& e, const LtShape& sh, const CUtensorMap* map_out, float* v,
@@ -203,13 +194,10 @@ __device__ __forceinline__ bool way_out(WayOut& w, const LinEpilogue& e, const L
           for (int i = 0; i < 8; ++i) v[j + i] += r[i];
         }
       }
-      store_row32(e, sh, v, row, col);
+#pragma unroll
+      for (int j = 0; j < 32; j += 8)
+        if (j < left) store8(e.out, e.out_f32, (int64_t)row * e.ldo + col + j, sh.vec, left - j, v + j);
     }
-    return true;
-  }
-  const bool by_hand = sh.ragged && left < 32;       // the same for the whole warp
-  if (e.out_f32 && by_hand) {
-    store_row32(e, sh, v, row, col);
     return true;
   }
   if (e.out_f32) {
@@ -259,10 +247,9 @@ __device__ __forceinline__ bool way_out(WayOut& w, const LinEpilogue& e, const L
   fence_proxy_async();
   __syncwarp();
   if (lane == 0) {
-    if (row0 < sh.M && left > 0 && !by_hand) tma_store_2d(map_out, buf, col, row0);
+    if (row0 < sh.M && left > 0) tma_store_2d(map_out, buf, col, row0);
     tma_store_commit();
   }
-  if (by_hand) store_row32(e, sh, v, row, col);
   ++w.n;
   return true;
 }
@@ -1061,8 +1048,7 @@ sc_status launch(const LinProblem& p, unsigned* status, cudaStream_t s) {
     sh.m_fastest = p.M <= p.N;
     if (!encode_operand(&a, p.A, p.M, p.K, 128) || !encode_operand(&b, p.B, p.N, p.K, c.bn / 2)) return SC_ERR_CUDA;
     CUtensorMap o = a, r = a;          // placeholders where the epilogue does not go through shared memory
-    sh.staged = sh.vec && !(p.epi.out_f32 && p.epi.res);
-    sh.ragged = sh.staged && p.N * es % 16 != 0;
+    sh.staged = sh.vec && p.N * es % 16 == 0 && !(p.epi.out_f32 && p.epi.res);
     if (sh.staged) {
       if (!encode(&o, p.epi.out, p.N, p.M, p.epi.ldo, 32, p.epi.out_f32 ? 16 : 32, CU_TENSOR_MAP_SWIZZLE_64B, p.epi.out_f32))
         return SC_ERR_CUDA;
